@@ -231,6 +231,62 @@ int  cadmm_op_wgrad_noalloc(cadmm_ctx* ctx, const float* A, const float* G, int6
                             float* out);
 
 /*
+ * Products over groups of rows, each group with a matrix of its own (weights per community; rows routed to an expert): group g owns
+ * the rows [group_ptr[g], group_ptr[g+1]) of A, G and out, 0 <= group_ptr[0] <= ... <= group_ptr[n_groups] <= n, a DEVICE array of
+ * n_groups + 1 numbers that the kernels read, so that it may come from an earlier kernel of the stream.  Groups may be empty.  Rows before
+ * group_ptr[0] and from group_ptr[n_groups] on belong to no group: they are not read, and those of out are left as they are.
+ * (Bounds are clamped to [0, n]; with descending ones the results are unspecified, but no other memory is touched.)
+ * The communities of a graph are such groups: comm_row_ptr of cadmm_get_graph, rows in the internal order.
+ *   transform_grouped:  out[r] = A[r] B_g        A device n x K, out device n x C; B device n_groups x K x C, or with b_transposed
+ *                       n_groups x C x K and B_g the transpose of what is stored: the gradient with respect to the left operand of the
+ *                       untransposed product is the transposed one of out's gradient with the same B
+ *   wgrad_grouped:      out_g = A_g^T G_g        A device n x K, G device n x C; out device n_groups x K x C, the gradient with
+ *                       respect to B; a group without rows gets zeros
+ * type: of A, B, G and of out (wgrad_grouped: out_type, the same or CADMM_F32).  lda, ldg, ldo: elements from one row to the next, at least
+ * the row's length; B and wgrad_grouped's out are dense.  Pointers need the alignment of their elements only.  Outputs overlap neither
+ * inputs nor each other.  Products are summed in fp32 and rounded once; fp32 operands count with all 24 bits of their significands.  An
+ * operand that is not finite makes the results that it enters not finite (rows of other groups, and rows past the last, enter none).
+ * No atomics: the same call gives the same bits.  n = 0 is allowed (A, G and transform_grouped's out may then be null).
+ * wgrad_grouped needs device scratch of _scratch bytes, 256-byte aligned, that no other call uses until it is done; nothing in
+ * it has to be cleared.  Neither call needs a graph, model or workspace.  Both run on the stream of the kernel-level calls and make the
+ * context's device current for themselves.  At most 65536 columns and 2^20 groups.
+ */
+#define CADMM_F32  0
+#define CADMM_BF16 1
+#define CADMM_F16  2
+int  cadmm_op_transform_grouped(cadmm_ctx* ctx, int32_t type, const void* A, int64_t n, int64_t lda, int32_t K, const void* B,
+                                int32_t C, int32_t b_transposed, int32_t n_groups, const int64_t* group_ptr, void* out,
+                                int64_t ldo);
+int  cadmm_op_wgrad_grouped_scratch(cadmm_ctx* ctx, int64_t n, int32_t K, int32_t C, int32_t n_groups, size_t* bytes);
+int  cadmm_op_wgrad_grouped(cadmm_ctx* ctx, int32_t type, const void* A, int64_t n, int64_t lda, int32_t K, const void* G, int64_t ldg,
+                            int32_t C, int32_t n_groups, const int64_t* group_ptr, int32_t out_type, void* out,
+                            void* scratch, size_t scratch_bytes);
+
+/*
+ * Orthogonalised updates of a stack of weights (no counterpart in the paper, whose W step follows the gradient itself; the stack
+ * is what wgrad_grouped leaves, or one gradient of cadmm_op_wgrad with batch = 1).
+ *   orthogonalise:  for every matrix of G (device batch x K x C, dense, of `type`): X = G / (||G||_F + eps), then `steps` times
+ *                   X <- a X + (b S + c S^2) X,  S = X X^T (K <= C; else the same of the transpose), coefficients = host {a, b, c}:
+ *                   singular vectors stay, a singular value x becomes a x + b x^3 + c x^5.  out: device, as G.  A zero matrix gives
+ *                   zeros (with eps = 0 too), one with an entry that is not finite NaNs throughout; the other matrices are not
+ *                   concerned.  Entries of X are held to 2^-36 of one: of a G far below eps, little is left.  out may be G itself; it overlaps it in no other way.
+ *   muon_step:      M <- momentum M + G;  D = G + momentum M with nesterov, else M;  W <- (1 - lr weight_decay) W - lr scale O with
+ *                   O the orthogonalised D.  W, M: device batch x K x C, fp32, updated in place; G of `type`, not changed.  The three
+ *                   do not overlap.
+ * 1 <= steps <= 64; eps >= 0; coefficients under which a singular value in [0, 1] could grow past 1024 on the way are CADMM_EINVAL.  Products take
+ * their operands with at least 22 bits and are summed in fp32, norms in fp64.  No atomics: the same call gives the
+ * same bits.  scratch: device, _scratch bytes, 256-byte aligned, used by no other call until this one is done; nothing in it has to be
+ * cleared.  Neither call needs a graph, model or workspace; streams and devices as for the products over groups.  At most 32768 rows or
+ * columns and 65535 matrices (CADMM_EUNSUPPORTED).
+ */
+int  cadmm_op_orthogonalise_scratch(cadmm_ctx* ctx, int32_t batch, int32_t K, int32_t C, size_t* bytes);
+int  cadmm_op_orthogonalise(cadmm_ctx* ctx, int32_t type, const void* G, int32_t batch, int32_t K, int32_t C, int32_t steps,
+                            const float* coefficients, float eps, void* out, void* scratch, size_t scratch_bytes);
+int  cadmm_op_muon_step(cadmm_ctx* ctx, int32_t type, const void* G, float* W, float* M, int32_t batch, int32_t K, int32_t C, float lr,
+                        float momentum, int32_t nesterov, float weight_decay, float scale, int32_t steps,
+                        const float* coefficients, float eps, void* scratch, size_t scratch_bytes);
+
+/*
  * Machine calibration for the rooflines the benchmarks quote (no counterpart in the paper).  Runs `reps` timed
  * launches (after one untimed) on the context's stream, synchronises, and returns the rate.
  *   kind 0: plain copy of `count` floats (multiple of 4) from src to dst, both device; rate = GB/s read + written.

@@ -24,6 +24,8 @@ EXPORTS = [
     "cadmm_op_aggregate_segments", "cadmm_op_transform", "cadmm_op_wgrad",
     "cadmm_profile", "cadmm_get_profile", "cadmm_profile_class_name", "cadmm_tune", "cadmm_predict",
     "cadmm_partition", "cadmm_op_calibrate", "cadmm_op_wgrad_noalloc", "cadmm_get_fista", "cadmm_op_stream",
+    "cadmm_op_transform_grouped", "cadmm_op_wgrad_grouped_scratch", "cadmm_op_wgrad_grouped",
+    "cadmm_op_orthogonalise_scratch", "cadmm_op_orthogonalise", "cadmm_op_muon_step",
 ]
 PROFILE_CLASSES = 19
 
@@ -91,6 +93,13 @@ def load_library():
     lib.cadmm_op_wgrad.argtypes = [vp, vp, vp, i64, i32, i32, vp]
     lib.cadmm_op_wgrad_noalloc.argtypes = [vp, vp, vp, i64, i32, i32, vp]
     lib.cadmm_op_stream.argtypes = [vp, vp]
+    f32, sizep = C.c_float, C.POINTER(C.c_size_t)
+    lib.cadmm_op_transform_grouped.argtypes = [vp, i32, vp, i64, i64, i32, vp, i32, i32, i32, vp, vp, i64]
+    lib.cadmm_op_wgrad_grouped_scratch.argtypes = [vp, i64, i32, i32, i32, sizep]
+    lib.cadmm_op_wgrad_grouped.argtypes = [vp, i32, vp, i64, i64, i32, vp, i64, i32, i32, vp, i32, vp, vp, C.c_size_t]
+    lib.cadmm_op_orthogonalise_scratch.argtypes = [vp, i32, i32, i32, sizep]
+    lib.cadmm_op_orthogonalise.argtypes = [vp, i32, vp, i32, i32, i32, i32, vp, f32, vp, vp, C.c_size_t]
+    lib.cadmm_op_muon_step.argtypes = [vp, i32, vp, vp, vp, i32, i32, i32, f32, f32, i32, f32, f32, i32, vp, f32, vp, C.c_size_t]
     lib.cadmm_op_calibrate.argtypes = [vp, i32, vp, vp, i64, i32, C.POINTER(C.c_double)]
     lib.cadmm_tune.argtypes = [vp, C.c_char_p, i32]
     lib.cadmm_predict.argtypes = [vp, vp, vp, C.POINTER(C.c_double)]
@@ -396,6 +405,131 @@ class Solver:
         self._check(self.lib.cadmm_op_wgrad_noalloc(self.h, A.data_ptr(), G.data_ptr(), A.shape[0], A.shape[1],
                                                     G.shape[1], out.data_ptr()), "cadmm_op_wgrad_noalloc")
         return out
+
+    # products over groups of rows and orthogonalised updates: fp32, bf16 and fp16 device tensors of this solver's GPU
+    def _device_tensors(self, what, **tensors):
+        for name, t in tensors.items():
+            if not t.is_cuda or t.device.index != self.device:
+                raise CadmmError(f"{what}: {name} is not on GPU {self.device}")
+
+    def _rows(self, what, name, t, types):
+        """Row stride of a matrix whose rows are dense."""
+        if t.dtype not in types:
+            raise CadmmError(f"{what}: {name} has type {t.dtype}")
+        if t.dim() != 2 or t.shape[1] < 1 or (t.shape[0] > 0 and t.shape[1] > 1 and t.stride(1) != 1):
+            raise CadmmError(f"{what}: {name} must be a matrix with dense rows")
+        return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+    def _stack(self, what, name, t, shape, types):
+        if t.dtype not in types:
+            raise CadmmError(f"{what}: {name} has type {t.dtype}")
+        if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+            raise CadmmError(f"{what}: {name} must be dense of shape {tuple(shape)}")
+
+    def _value_types(self):
+        torch = self._torch
+        return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+    def _scratch(self, query, *args):
+        """Scratch of one call, from torch's allocator for the current stream: (aligned pointer, bytes, what keeps it alive)."""
+        nbytes = C.c_size_t()
+        self._check(query(self.h, *args, C.byref(nbytes)), query.__name__)
+        if nbytes.value == 0:
+            return None, 0, None
+        hold = self._torch.empty(nbytes.value + 255, dtype=self._torch.uint8, device=f"cuda:{self.device}")
+        return (hold.data_ptr() + 255) & ~255, nbytes.value, hold
+
+    def op_transform_grouped(self, A, B, group_ptr, transposed=False, out=None):
+        """out[r] = A[r] B_g for the rows r in [group_ptr[g], group_ptr[g + 1]) of every group.  A: n x K, B: groups x K x C
+        (transposed: groups x C x K, and B_g is its transpose), group_ptr: int64 device tensor of groups + 1 bounds that do not
+        descend.  `out` may be a preallocated n x C matrix with dense rows: rows of no group are left as they are there, and
+        hold anything otherwise.  With the communities' weights in B: group_ptr = comm_row_ptr of get_graph."""
+        torch, what, types = self._torch, "op_transform_grouped", self._value_types()
+        self._device_tensors(what, A=A, B=B, group_ptr=group_ptr)
+        lda = self._rows(what, "A", A, types)
+        n, K = A.shape
+        groups = group_ptr.shape[0] - 1 if group_ptr.dim() == 1 else 0
+        if groups < 1:
+            raise CadmmError(f"{what}: group_ptr must hold groups + 1 bounds")
+        self._stack(what, "group_ptr", group_ptr, (groups + 1,), (torch.int64,))
+        width = B.shape[1 if transposed else 2] if B.dim() == 3 else 0
+        self._stack(what, "B", B, (groups, width, K) if transposed else (groups, K, width), (A.dtype,))
+        if out is None:
+            out = torch.empty((n, width), dtype=A.dtype, device=A.device)
+        self._device_tensors(what, out=out)
+        ldo = self._rows(what, "out", out, (A.dtype,))
+        if tuple(out.shape) != (n, width):
+            raise CadmmError(f"{what}: out must be {n} x {width}")
+        self._on_current_stream()
+        self._check(self.lib.cadmm_op_transform_grouped(self.h, types[A.dtype], A.data_ptr(), n, lda, K, B.data_ptr(), width,
+                                                        int(bool(transposed)), groups, group_ptr.data_ptr(), out.data_ptr(), ldo),
+                    "cadmm_op_transform_grouped")
+        return out
+
+    def op_wgrad_grouped(self, A, G, group_ptr, out=None, out_dtype=None):
+        """out[g] = A_g^T G_g over the rows of every group (groups x K x C): the gradient of op_transform_grouped with respect to
+        B.  In fp32 unless `out` or out_dtype (fp32 or the operands' type) says otherwise; zeros for a group without rows."""
+        torch, what, types = self._torch, "op_wgrad_grouped", self._value_types()
+        self._device_tensors(what, A=A, G=G, group_ptr=group_ptr)
+        lda, ldg = self._rows(what, "A", A, types), self._rows(what, "G", G, (A.dtype,))
+        if A.shape[0] != G.shape[0]:
+            raise CadmmError(f"{what}: A and G have different numbers of rows")
+        groups = group_ptr.shape[0] - 1 if group_ptr.dim() == 1 else 0
+        if groups < 1:
+            raise CadmmError(f"{what}: group_ptr must hold groups + 1 bounds")
+        self._stack(what, "group_ptr", group_ptr, (groups + 1,), (torch.int64,))
+        (n, K), width = A.shape, G.shape[1]
+        if out is None:
+            out = torch.empty((groups, K, width), dtype=out_dtype or torch.float32, device=A.device)
+        self._device_tensors(what, out=out)
+        self._stack(what, "out", out, (groups, K, width), (torch.float32, A.dtype) if out_dtype is None else (out_dtype,))
+        ptr, nbytes, hold = self._scratch(self.lib.cadmm_op_wgrad_grouped_scratch, n, K, width, groups)
+        self._on_current_stream()
+        self._check(self.lib.cadmm_op_wgrad_grouped(self.h, types[A.dtype], A.data_ptr(), n, lda, K, G.data_ptr(), ldg, width, groups,
+                                                    group_ptr.data_ptr(), types.get(out.dtype, -1), out.data_ptr(), ptr, nbytes),
+                    "cadmm_op_wgrad_grouped")
+        return out
+
+    def op_orthogonalise(self, G, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, out=None):
+        """G (K x C, or a stack batch x K x C) with the singular values of every matrix brought towards one: `steps` times
+        X <- a X + (b S + c S^2) X, S = X X^T, from X = G / (||G||_F + eps).  `out` may be G itself."""
+        torch, what, types = self._torch, "op_orthogonalise", self._value_types()
+        out = torch.empty_like(G, memory_format=torch.contiguous_format) if out is None else out
+        self._device_tensors(what, G=G, out=out)
+        batch, K, width = self._matrices(what, G)
+        self._stack(what, "G", G, G.shape, types)
+        self._stack(what, "out", out, G.shape, (G.dtype,))
+        ptr, nbytes, hold = self._scratch(self.lib.cadmm_op_orthogonalise_scratch, batch, K, width)
+        self._on_current_stream()
+        self._check(self.lib.cadmm_op_orthogonalise(self.h, types[G.dtype], G.data_ptr(), batch, K, width, steps, self._coefficients(coefficients),
+                                                    eps, out.data_ptr(), ptr, nbytes), "cadmm_op_orthogonalise")
+        return out
+
+    def op_muon_step(self, W, M, G, *, lr, momentum=0.95, nesterov=True, weight_decay=0.0, scale=1.0, steps=5,
+                     coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7):
+        """One optimiser step on W (K x C, or a stack), in place: M <- momentum M + G, D = G + momentum M (nesterov) or M,
+        W <- (1 - lr weight_decay) W - lr scale O with O the orthogonalised D.  W and M are fp32."""
+        torch, what, types = self._torch, "op_muon_step", self._value_types()
+        self._device_tensors(what, W=W, M=M, G=G)
+        batch, K, width = self._matrices(what, G)
+        self._stack(what, "G", G, G.shape, types)
+        self._stack(what, "W", W, G.shape, (torch.float32,))
+        self._stack(what, "M", M, G.shape, (torch.float32,))
+        ptr, nbytes, hold = self._scratch(self.lib.cadmm_op_orthogonalise_scratch, batch, K, width)
+        self._on_current_stream()
+        self._check(self.lib.cadmm_op_muon_step(self.h, types[G.dtype], G.data_ptr(), W.data_ptr(), M.data_ptr(), batch, K, width, lr, momentum,
+                                                int(bool(nesterov)), weight_decay, scale, steps, self._coefficients(coefficients), eps, ptr, nbytes),
+                    "cadmm_op_muon_step")
+
+    def _coefficients(self, coefficients):
+        if len(coefficients) != 3:
+            raise CadmmError("three coefficients are wanted")
+        return (C.c_float * 3)(*coefficients)
+
+    def _matrices(self, what, G):
+        if G.dim() not in (2, 3) or G.numel() == 0:
+            raise CadmmError(f"{what}: G must be a matrix or a stack of matrices")
+        return (1 if G.dim() == 2 else G.shape[0]), G.shape[-2], G.shape[-1]
 
     def tune(self, key, value):
         self._check(self.lib.cadmm_tune(self.h, key.encode(), int(value)), "cadmm_tune")

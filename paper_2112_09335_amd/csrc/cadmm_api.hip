@@ -1219,6 +1219,46 @@ int on_op_stream(cadmm_ctx* c, const char* what, F body) {
     return check_launch(c, what);
 }
 
+// Kernel-level calls that make the context's device current for their launches, whichever is current for the calling thread.
+template <class F>
+int on_own_device(cadmm_ctx* c, const char* what, F body) {
+    int current = -1;
+    HIP_TRY(c, hipGetDevice(&current));
+    if (current != c->device) HIP_TRY(c, hipSetDevice(c->device));
+    const int rc = on_op_stream(c, what, body);
+    if (current != c->device) (void)hipSetDevice(current);
+    return rc;
+}
+
+size_t type_bytes(int32_t type) { return type == CADMM_F32 ? 4 : 2; }
+bool known_type(int32_t type) { return type == CADMM_F32 || type == CADMM_BF16 || type == CADMM_F16; }
+bool misaligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
+
+constexpr int64_t kMostWidth = 1 << 16, kMostGroups = 1 << 20, kMostRows = (int64_t)1 << 40, kMostBlocks = 0x7fffffff;
+constexpr float kMostGrowth = 1024.f;            // singular values of the polynomial's iterates
+
+// What the products over groups ask of their sizes; "" or what is wrong.
+const char* grouped_fault(int64_t n, int64_t lda, int32_t K, int64_t ldc, int32_t C, int32_t groups) {
+    if (n > kMostRows) return "too many rows";
+    if (K > kMostWidth || C > kMostWidth) return "more than 65536 columns";
+    if (groups > kMostGroups) return "more than 2^20 groups";
+    if (lda < K || ldc < C) return "rows overlap: a row stride is less than the row's length";
+    if (n > 0 && (lda > ((int64_t)1 << 60) / n || ldc > ((int64_t)1 << 60) / n)) return "row strides beyond the address space";
+    return "";
+}
+
+// The largest singular value of the iterates after `steps` applications of x (a + b x^2 + c x^4) to values in [0, 1]; growth[k]: the
+// bound before step k.  A value that is not finite comes back as such.
+double polynomial_growth(double a, double b, double c, int steps) {
+    double s = 1.0, most = 1.0;
+    for (int k = 0; k < steps; ++k) {
+        s = polynomial_bound(a, b, c, s);
+        if (!(s <= most)) most = s;
+        if (!(s <= 1e6)) return s;
+    }
+    return most;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1873,6 +1913,107 @@ int cadmm_op_wgrad_noalloc(cadmm_ctx* c, const float* A, const float* G, int64_t
     const int rc = on_op_stream(c, "op_wgrad_noalloc", [&] { launch_gemm_tn(c->stream, A, G, out, n, K, C, ptr); });
     if (current != c->device) (void)hipSetDevice(current);
     return rc;
+}
+
+int cadmm_op_transform_grouped(cadmm_ctx* c, int32_t type, const void* A, int64_t n, int64_t lda, int32_t K, const void* B, int32_t C,
+                               int32_t b_transposed, int32_t n_groups, const int64_t* group_ptr, void* out, int64_t ldo) {
+    if (!c || !B || !group_ptr || n < 0 || (n > 0 && (!A || !out)) || K < 1 || C < 1 || n_groups < 1) return CADMM_EINVAL;
+    if (!known_type(type)) return fail(c, CADMM_EINVAL, "type must be CADMM_F32, CADMM_BF16 or CADMM_F16");
+    const char* fault = grouped_fault(n, lda, K, ldo, C, n_groups);
+    if (*fault) return fail(c, CADMM_EINVAL, fault);
+    const size_t bytes = type_bytes(type);
+    if (misaligned(A, bytes) || misaligned(B, bytes) || misaligned(out, bytes) || misaligned(group_ptr, 8))
+        return fail(c, CADMM_EINVAL, "a pointer is not aligned to its elements");
+    if (c->device < 0) return fail(c, CADMM_EUNSUPPORTED, "host-only context (device -1) has no device path");
+    if (grouped_nn_blocks(n, C, n_groups) > kMostBlocks) return fail(c, CADMM_EUNSUPPORTED, "more result tiles than one launch holds");
+    if (n == 0) return CADMM_OK;
+    const GroupedNN args{A, n, lda, K, B, C, b_transposed != 0, n_groups, group_ptr, out, ldo};
+    return on_own_device(c, "op_transform_grouped", [&] {
+        timed(c, P_OTHER, (double)bytes * ((double)n * K + (double)n * C + (double)std::min<int64_t>(n, n_groups) * K * C) + 8.0 * (n_groups + 1.0),
+              2.0 * (double)n * K * C, [&] { launch_grouped_nn(c->stream, type, args); });
+    });
+}
+
+int cadmm_op_wgrad_grouped_scratch(cadmm_ctx* c, int64_t n, int32_t K, int32_t C, int32_t n_groups, size_t* bytes) {
+    if (!c || !bytes || n < 0 || K < 1 || C < 1 || n_groups < 1) return CADMM_EINVAL;
+    const char* fault = grouped_fault(n, K, K, C, C, n_groups);
+    if (*fault) return fail(c, CADMM_EINVAL, fault);
+    *bytes = grouped_tn_scratch(n, K, C, n_groups);
+    return CADMM_OK;
+}
+
+int cadmm_op_wgrad_grouped(cadmm_ctx* c, int32_t type, const void* A, int64_t n, int64_t lda, int32_t K, const void* G, int64_t ldg, int32_t C,
+                           int32_t n_groups, const int64_t* group_ptr, int32_t out_type, void* out, void* scratch, size_t scratch_bytes) {
+    if (!c || !out || !group_ptr || n < 0 || (n > 0 && (!A || !G)) || K < 1 || C < 1 || n_groups < 1) return CADMM_EINVAL;
+    if (!known_type(type) || (out_type != CADMM_F32 && out_type != type))
+        return fail(c, CADMM_EINVAL, "type must be CADMM_F32, CADMM_BF16 or CADMM_F16, out_type the same or CADMM_F32");
+    const char* fault = grouped_fault(n, lda, K, ldg, C, n_groups);
+    if (*fault) return fail(c, CADMM_EINVAL, fault);
+    const size_t bytes = type_bytes(type), need = grouped_tn_scratch(n, K, C, n_groups);
+    if (misaligned(A, bytes) || misaligned(G, bytes) || misaligned(out, type_bytes(out_type)) || misaligned(group_ptr, 8))
+        return fail(c, CADMM_EINVAL, "a pointer is not aligned to its elements");
+    if (need > 0 && (!scratch || misaligned(scratch, 256))) return fail(c, CADMM_EINVAL, "scratch must be 256-byte aligned");
+    if (scratch_bytes < need) return fail(c, CADMM_ENOMEM, "scratch is smaller than cadmm_op_wgrad_grouped_scratch says");
+    if (c->device < 0) return fail(c, CADMM_EUNSUPPORTED, "host-only context (device -1) has no device path");
+    if (grouped_tn_blocks(n, K, C, n_groups) > kMostBlocks) return fail(c, CADMM_EUNSUPPORTED, "more result tiles than one launch holds");
+    const GroupedTN args{A, n, lda, K, G, ldg, C, n_groups, group_ptr, out, scratch};
+    return on_own_device(c, "op_wgrad_grouped", [&] {
+        timed(c, P_OTHER, (double)bytes * ((double)n * K + (double)n * C) + (double)type_bytes(out_type) * n_groups * K * C + 8.0 * (n_groups + 1.0),
+              2.0 * (double)n * K * C, [&] { launch_grouped_tn(c->stream, type, out_type, args); });
+    });
+}
+
+int cadmm_op_orthogonalise_scratch(cadmm_ctx* c, int32_t batch, int32_t K, int32_t C, size_t* bytes) {
+    if (!c || !bytes || batch < 1 || K < 1 || C < 1) return CADMM_EINVAL;
+    const char* fault = orthogonal_fault(batch, K, C);
+    if (*fault) return fail(c, CADMM_EUNSUPPORTED, fault);
+    *bytes = orthogonal_scratch(batch, K, C);
+    return CADMM_OK;
+}
+
+namespace {
+int orthogonalise(cadmm_ctx* c, const char* what, int32_t type, Orthogonal a, const float* coefficients, size_t scratch_bytes) {
+    const char* fault = orthogonal_fault(a.batch, a.K, a.C);
+    if (*fault) return fail(c, CADMM_EUNSUPPORTED, fault);
+    if (!known_type(type)) return fail(c, CADMM_EINVAL, "type must be CADMM_F32, CADMM_BF16 or CADMM_F16");
+    if (a.steps < 1 || a.steps > 64) return fail(c, CADMM_EINVAL, "steps must be in [1, 64]");
+    if (!(a.eps >= 0.f) || !std::isfinite(a.eps)) return fail(c, CADMM_EINVAL, "eps must be finite and not negative");
+    a.a = coefficients[0]; a.b = coefficients[1]; a.c = coefficients[2];
+    if (!(polynomial_growth(a.a, a.b, a.c, a.steps) <= kMostGrowth))
+        return fail(c, CADMM_EINVAL, "with these coefficients singular values could grow past 1024");
+    const size_t bytes = type_bytes(type);
+    if (misaligned(a.G, bytes) || misaligned(a.out, bytes) || misaligned(a.W, 4) || misaligned(a.M, 4))
+        return fail(c, CADMM_EINVAL, "a pointer is not aligned to its elements");
+    if (misaligned(a.scratch, 256)) return fail(c, CADMM_EINVAL, "scratch must be 256-byte aligned");
+    if (scratch_bytes < orthogonal_scratch(a.batch, a.K, a.C)) return fail(c, CADMM_ENOMEM, "scratch is smaller than cadmm_op_orthogonalise_scratch says");
+    if (c->device < 0) return fail(c, CADMM_EUNSUPPORTED, "host-only context (device -1) has no device path");
+    const double r = std::min(a.K, a.C), s = std::max(a.K, a.C), count = (double)a.batch * a.K * a.C;
+    return on_own_device(c, what, [&] {
+        timed(c, P_OTHER, count * (a.W ? (double)bytes + 16.0 : 2.0 * (double)bytes), (double)a.batch * a.steps * (3.0 * r * r * s + r * r * r),
+              [&] { launch_orthogonalise(c->stream, type, a); });
+    });
+}
+}  // namespace
+
+int cadmm_op_orthogonalise(cadmm_ctx* c, int32_t type, const void* G, int32_t batch, int32_t K, int32_t C, int32_t steps,
+                           const float* coefficients, float eps, void* out, void* scratch, size_t scratch_bytes) {
+    if (!c || !G || !out || !coefficients || !scratch || batch < 1 || K < 1 || C < 1) return CADMM_EINVAL;
+    Orthogonal a{};
+    a.G = G; a.batch = batch; a.K = K; a.C = C; a.steps = steps; a.eps = eps; a.out = out; a.scratch = scratch;
+    return orthogonalise(c, "op_orthogonalise", type, a, coefficients, scratch_bytes);
+}
+
+int cadmm_op_muon_step(cadmm_ctx* c, int32_t type, const void* G, float* W, float* M, int32_t batch, int32_t K, int32_t C, float lr, float momentum,
+                       int32_t nesterov, float weight_decay, float scale, int32_t steps, const float* coefficients, float eps, void* scratch,
+                       size_t scratch_bytes) {
+    if (!c || !G || !W || !M || !coefficients || !scratch || batch < 1 || K < 1 || C < 1) return CADMM_EINVAL;
+    for (float x : {lr, momentum, weight_decay, scale})
+        if (!std::isfinite(x)) return fail(c, CADMM_EINVAL, "lr, momentum, weight_decay and scale must be finite");
+    Orthogonal a{};
+    a.G = G; a.batch = batch; a.K = K; a.C = C; a.steps = steps; a.eps = eps; a.scratch = scratch;
+    a.W = W; a.M = M; a.mu = momentum; a.nesterov = nesterov != 0;
+    a.keep = (float)(1.0 - (double)lr * weight_decay); a.rate = (float)((double)lr * scale);
+    return orthogonalise(c, "op_muon_step", type, a, coefficients, scratch_bytes);
 }
 
 int cadmm_op_calibrate(cadmm_ctx* c, int32_t kind, const float* src, float* dst, int64_t count, int32_t reps,

@@ -186,6 +186,44 @@ int launch_gemm_tn(hipStream_t s, const float* A, const float* G, float* out, in
 // out[C x K] = in[K x C]^T (small)
 void launch_transpose(hipStream_t s, const float* in, float* out, int K, int C);
 
+// ---------------------------------------------------------------- products over groups of rows (grouped.hip)
+enum ValueType { kF32 = 0, kBf16 = 1, kF16 = 2 };
+// out[r] = A[r] B_g for the rows r in [ptr[g], ptr[g+1]) of every group; B: groups x K x C, or groups x C x K (transposed).
+struct GroupedNN {
+    const void* A; int64_t n, lda; int K;
+    const void* B; int C; bool transposed;
+    int groups; const int64_t* ptr;
+    void* out; int64_t ldo;
+};
+int64_t grouped_nn_blocks(int64_t n, int C, int groups);      // most workgroups of a launch
+void launch_grouped_nn(hipStream_t s, int type, const GroupedNN& a);
+// out_g = A_g^T G_g: groups x K x C, of the operands' type or fp32.
+struct GroupedTN {
+    const void* A; int64_t n, lda; int K;
+    const void* G; int64_t ldg; int C;
+    int groups; const int64_t* ptr;
+    void* out; void* scratch;
+};
+int64_t grouped_tn_blocks(int64_t n, int K, int C, int groups);
+size_t grouped_tn_scratch(int64_t n, int K, int C, int groups);
+void launch_grouped_tn(hipStream_t s, int type, int out_type, const GroupedTN& a);
+
+// ---------------------------------------------------------------- orthogonalised updates (orthogonal.hip)
+// batch matrices K x C of `type`.  Without W: out (of `type`) = the polynomial's result.  With W and M (fp32): M = mu M + G, the
+// direction is G + mu M (nesterov) or M, and W = keep W - rate * result.
+struct Orthogonal {
+    const void* G; int batch, K, C, steps;
+    float a, b, c, eps;
+    void* out;
+    float *W, *M; float mu, keep, rate; bool nesterov;
+    void* scratch;
+};
+// The largest |x (a + b x^2 + c x^4)| for x in [0, s] (infinite where it cannot be told).
+double polynomial_bound(double a, double b, double c, double s);
+const char* orthogonal_fault(int batch, int K, int C);        // "" or why such a stack is refused
+size_t orthogonal_scratch(int batch, int K, int C);
+void launch_orthogonalise(hipStream_t s, int type, const Orthogonal& a);
+
 // ---------------------------------------------------------------- fused elementwise + reductions (elementwise.hip)
 constexpr int kReduceBlocks = 2048;      // grid of the flat reducing kernels
 constexpr int kMaxCand = 16;             // step-size candidates evaluated at once in a later pass

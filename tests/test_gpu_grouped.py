@@ -1,0 +1,334 @@
+"""GPU parity of the products over groups of rows against products in 64 bits.
+
+Tolerances: a result is a sum of `depth` products.  Summed in fp32 in any order it is off by at most depth 2^-24 sum |a||b|; operands
+in three 8-bit parts leave out less than 3 * 2^-24 of every product, and an instruction's own sums of 8 to 32 products add a few roundings
+more: (depth + 8) 2^-24 sum |a||b| in all.  It is then rounded once: half a step of its type, or of the type's smallest number."""
+import numpy as np
+import pytest
+
+from paper_2112_09335_amd import synth
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def solver():
+    from paper_2112_09335_amd import binding
+    s = binding.Solver(0)                         # no graph, model or workspace
+    yield s
+    s.close()
+
+
+def types():
+    import torch
+    return {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+LEAST = {"f32": 2.0 ** -149, "bf16": 2.0 ** -133, "f16": 2.0 ** -24}
+
+
+def close(got, want, magnitude, depth, kind):
+    """got against the 64-bit result, magnitude = sum |a||b| of every entry."""
+    got = got.detach().cpu().double().numpy()
+    loose = (depth + 8) * 2.0 ** -24 * magnitude
+    room = loose + HALF[kind] * (np.abs(want) + loose) + LEAST[kind]
+    far = np.abs(got - want) - room
+    assert np.isfinite(got).all()
+    assert (far <= 0).all(), (far.max(), np.unravel_index(far.argmax(), far.shape), (np.abs(got - want) / np.maximum(room, 1e-300)).max())
+
+
+def draw(torch, seed, sizes, K, width, kind, transposed=False, before=0, behind=0, scale=1.0):
+    """Rows of `sizes` groups between `before` and `behind` rows of no group, as CPU tensors of the type."""
+    rng = np.random.default_rng(seed)
+    t = types()[kind]
+    n = before + int(sum(sizes)) + behind
+    A = torch.from_numpy(rng.standard_normal((n, K)).astype(np.float32) * scale).to(t)
+    B = torch.from_numpy(rng.standard_normal((len(sizes), width, K) if transposed else (len(sizes), K, width)).astype(np.float32)).to(t)
+    ptr = torch.from_numpy((before + np.concatenate([[0], np.cumsum(sizes)])).astype(np.int64))
+    return A, B, ptr
+
+
+def want_nn(A, B, ptr, transposed):
+    A, B, ptr = A.double().numpy(), B.double().numpy(), ptr.numpy()
+    out = np.zeros((A.shape[0], B.shape[1 if transposed else 2]))
+    size = np.zeros_like(out)
+    for g in range(len(ptr) - 1):
+        lo, hi = ptr[g], ptr[g + 1]
+        Bg = B[g].T if transposed else B[g]
+        out[lo:hi], size[lo:hi] = A[lo:hi] @ Bg, np.abs(A[lo:hi]) @ np.abs(Bg)
+    return out, size
+
+
+def want_tn(A, G, ptr):
+    A, G, ptr = A.double().numpy(), G.double().numpy(), ptr.numpy()
+    out = np.zeros((len(ptr) - 1, A.shape[1], G.shape[1]))
+    size = np.zeros_like(out)
+    for g in range(len(ptr) - 1):
+        lo, hi = ptr[g], ptr[g + 1]
+        out[g], size[g] = A[lo:hi].T @ G[lo:hi], np.abs(A[lo:hi]).T @ np.abs(G[lo:hi])
+    return out, size
+
+
+SHAPES = [
+    # groups' sizes, K, C
+    ([1], 1, 1), ([1], 64, 64), ([3], 5, 2), ([0, 1, 0], 33, 17), ([0, 0], 8, 8), ([1] * 70, 40, 24), ([5, 0, 130, 1, 64], 97, 301),
+    ([63, 64, 65], 64, 64), ([127, 128, 129, 0, 1], 128, 128), ([255, 256, 257], 256, 256), ([300, 5, 0, 700], 512, 320),
+    ([31, 2, 16, 15, 17, 8], 1000, 72), ([40, 33], 2048, 130), ([1000], 16, 3), ([2, 1, 0, 4], 1024, 512), ([600, 900], 7, 260),
+    ([1500, 20], 136, 136), ([513], 520, 264), ([16, 16, 1, 0, 3], 2048, 1024),
+]
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("sizes,K,width", SHAPES, ids=lambda v: str(v).replace(" ", "")[:24])
+def test_product_over_groups(solver, kind, transposed, sizes, K, width):
+    import torch
+    A, B, ptr = draw(torch, K + width, sizes, K, width, kind, transposed)
+    out = solver.op_transform_grouped(A.cuda(), B.cuda(), ptr.cuda(), transposed=transposed)
+    assert out.dtype == A.dtype and tuple(out.shape) == (A.shape[0], width)
+    close(out, *want_nn(A, B, ptr, transposed), K, kind)
+
+
+@pytest.mark.parametrize("kind,out_kind", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16"), ("f16", "f32"), ("f16", "f16")])
+@pytest.mark.parametrize("sizes,K,width", SHAPES + [([20000, 3, 9000], 64, 48), ([70000], 24, 5), ([4096, 4097], 256, 256), ([40000], 130, 130)],
+                         ids=lambda v: str(v).replace(" ", "")[:24])
+def test_weight_gradient_over_groups(solver, kind, out_kind, sizes, K, width):
+    import torch
+    A, _, ptr = draw(torch, K + width, sizes, K, 1, kind)
+    G, _, _ = draw(torch, K + width + 1, sizes, width, 1, kind, scale=2.0 ** -5)
+    out = solver.op_wgrad_grouped(A.cuda(), G.cuda(), ptr.cuda(), out_dtype=types()[out_kind])
+    assert out.dtype == types()[out_kind]
+    close(out, *want_tn(A, G, ptr), max(sizes), out_kind)
+    again = solver.op_wgrad_grouped(A.cuda(), G.cuda(), ptr.cuda(), out_dtype=types()[out_kind])
+    assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("K,width,step_a,step_o,at", [(64, 64, 64, 64, 0), (64, 64, 72, 80, 8), (64, 64, 65, 67, 1), (97, 301, 99, 303, 3), (256, 136, 256, 136, 1)])
+def test_strides_offsets_and_rows_of_no_group(solver, kind, transposed, K, width, step_a, step_o, at):
+    """A and out are parts of wider matrices, at any element; rows before the first group and behind the last are neither read (they hold no
+    numbers) nor written, and neither is anything between the rows."""
+    import torch
+    sizes = [70, 0, 33, 1, 150]
+    A, B, ptr = draw(torch, 5, sizes, K, width, kind, transposed, before=9, behind=40)
+    n = A.shape[0]
+    A[:9], A[-40:] = float("nan"), float("inf")
+    wide = torch.full((n * step_a + at + 8,), float("nan"), dtype=A.dtype, device="cuda")
+    Av = torch.as_strided(wide, (n, K), (step_a, 1), at)
+    Av.copy_(A)
+    held = torch.full((n * step_o + at + 8,), 7.0, dtype=A.dtype, device="cuda")
+    out = torch.as_strided(held, (n, width), (step_o, 1), at)
+    Bw = torch.zeros(B.numel() + at, dtype=B.dtype, device="cuda")[at:].view(B.shape)
+    Bw.copy_(B)
+    solver.op_transform_grouped(Av, Bw, ptr.cuda(), transposed=transposed, out=out)
+    want, size = want_nn(A, B, ptr, transposed)
+    close(out[9:-40], want[9:-40], size[9:-40], K, kind)
+    mask = torch.ones_like(held, dtype=torch.bool)
+    torch.as_strided(mask, (n, width), (step_o, 1), at)[9:-40] = False
+    assert (held[mask] == 7.0).all()
+    G, _, _ = draw(torch, 6, sizes, width, 1, kind, before=9, behind=40)
+    G[:9], G[-40:] = float("inf"), float("nan")
+    Gv = torch.as_strided(torch.full((n * step_o + at + 8,), float("nan"), dtype=A.dtype, device="cuda"), (n, width), (step_o, 1), at)
+    Gv.copy_(G)
+    dB = torch.full((len(sizes) * K * width + at,), 7.0, device="cuda")
+    solver.op_wgrad_grouped(Av, Gv, ptr.cuda(), out=dB[at:].view(len(sizes), K, width))
+    close(dB[at:].view(len(sizes), K, width), *want_tn(A, G, ptr), 150, "f32")
+    assert (dB[:at] == 7.0).all()
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("K,width", [(64, 64), (97, 41), (256, 256), (1024, 128)])
+def test_what_is_not_finite_stays_in_its_row_and_group(solver, kind, K, width):
+    import torch
+    sizes = [40, 3, 200, 17, 64]
+    A, B, ptr = draw(torch, 8, sizes, K, width, kind)
+    G, _, _ = draw(torch, 9, sizes, width, 1, kind)
+    want, size = want_nn(A, B, ptr, False)
+    dwant, dsize = want_tn(A, G, ptr)
+    A[41, K - 1], A[250, 0], B[3, K // 2, 1] = float("nan"), float("inf"), float("-inf")
+    out = solver.op_transform_grouped(A.cuda(), B.cuda(), ptr.cuda()).cpu()
+    bad = ~torch.isfinite(out)
+    lone = torch.zeros_like(bad)
+    lone[41], lone[250], lone[243:260, 1] = True, True, True        # rows 243 .. 259 are group 3
+    assert torch.equal(bad, lone)
+    keep = ~(lone.any(1) | lone.all(1)).numpy()
+    close(out[keep], want[keep], size[keep], K, kind)
+    dB = solver.op_wgrad_grouped(A.cuda(), G.cuda(), ptr.cuda()).cpu()
+    # row 41 is in group 1, row 250 in group 3: a row of dB each
+    bad = ~torch.isfinite(dB)
+    lone = torch.zeros_like(bad)
+    lone[1, K - 1], lone[3, 0] = True, True
+    assert torch.equal(bad, lone)
+    for g in (0, 2, 4):
+        close(dB[g], dwant[g], dsize[g], max(sizes), "f32")
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_many_groups(solver, kind):
+    """More groups than one step of the search looks at, most of them empty, and runs of equal bounds across its steps."""
+    import torch
+    rng = np.random.default_rng(3)
+    sizes = np.where(rng.random(5000) < 0.7, 0, rng.integers(0, 6, 5000))
+    sizes[1000:1400] = 0
+    sizes[4097] = 400
+    A, B, ptr = draw(torch, 11, sizes.tolist(), 24, 16, kind)
+    close(solver.op_transform_grouped(A.cuda(), B.cuda(), ptr.cuda()), *want_nn(A, B, ptr, False), 24, kind)
+    G, _, _ = draw(torch, 12, sizes.tolist(), 16, 1, kind)
+    close(solver.op_wgrad_grouped(A.cuda(), G.cuda(), ptr.cuda()), *want_tn(A, G, ptr), 400, "f32")
+
+
+def test_bounds_past_the_rows_are_clamped(solver):
+    """Bounds below zero and past n count as 0 and n; with descending ones the rows that two groups claim may hold either's product, and
+    nothing outside is touched."""
+    import torch
+    A, B, _ = draw(torch, 13, [200], 64, 64, "f32")
+    Bs = B.repeat(3, 1, 1)
+    want, size = want_nn(A, Bs, torch.tensor([0, 60, 200, 200]), False)
+    for ptr in ([-5, 60, 200, 900], [-(1 << 62), 60, 1 << 62, 1 << 62]):
+        held = torch.full((202, 64), 3.0, device="cuda")
+        solver.op_transform_grouped(A.cuda(), Bs.cuda(), torch.tensor(ptr).cuda(), out=held[1:201])
+        close(held[1:201], want, size, 64, "f32")
+        assert (held[0] == 3.0).all() and (held[201] == 3.0).all()
+        dB = solver.op_wgrad_grouped(A.cuda(), A.cuda(), torch.tensor(ptr).cuda())
+        close(dB, *want_tn(A, A, torch.tensor([0, 60, 200, 200])), 200, "f32")
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_offsets_past_32_bits(solver, kind):
+    """Rows so far apart that an element's offset passes 2^31 and a byte's 2^32, and as many results."""
+    import torch
+    n, step = 40000, 60000
+    A, B, ptr = draw(torch, 14, [1, 39990, 9], 32, 40, kind)
+    pick = np.r_[0:5, 20000:20005, n - 12:n]
+    big = torch.empty(n * step, dtype=A.dtype, device="cuda")
+    Av = torch.as_strided(big, (n, 32), (step, 1))
+    Av.copy_(A)
+    out = torch.as_strided(big, (n, 40), (step, 1), 64)
+    solver.op_transform_grouped(Av, B.cuda(), ptr.cuda(), out=out)
+    want, size = want_nn(A, B, ptr, False)
+    close(out[pick], want[pick], size[pick], 32, kind)
+    dB = solver.op_wgrad_grouped(Av, out, ptr.cuda())
+    close(dB, *want_tn(A, out.cpu(), ptr), 39990, "f32")
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_gradients_against_the_formulas_and_against_differences(solver, kind):
+    """L = sum D * (A_g B_g): dA = D B_g^T, dB_g = A_g^T D, and L is linear in either operand, so that (L(B + E) - L(B - E)) / 2 is the
+    directional derivative itself.  It is taken in 64 bits of products of the operator, whose roundings are counted."""
+    import torch
+    sizes, K, width = [50, 0, 81, 7], 72, 40
+    A, B, ptr = draw(torch, 21, sizes, K, width, kind)
+    D, _, _ = draw(torch, 22, sizes, width, 1, kind)
+    run = lambda X, Y: solver.op_transform_grouped(X.cuda(), Y.cuda(), ptr.cuda()).cpu().double()  # noqa: E731
+    dA = solver.op_transform_grouped(D.cuda(), B.cuda(), ptr.cuda(), transposed=True)
+    dB = solver.op_wgrad_grouped(A.cuda(), D.cuda(), ptr.cuda())
+    close(dA, *want_nn(D, B, ptr, True), width, kind)
+    close(dB, *want_tn(A, D, ptr), max(sizes), "f32")
+    rng = np.random.default_rng(23)
+    for X, grad in ((A, dA), (B, dB)):
+        # steps that the type holds exactly: powers of two of X's own step, with X rounded to leave room for them
+        E = torch.from_numpy(rng.choice([-1.0, 1.0], size=tuple(X.shape))).to(X.dtype)
+        near = (X * 4).round() / 4                       # X +- 1 is exact in every type
+        up = run(near + E, B) if X is A else run(A, near + E)
+        down = run(near - E, B) if X is A else run(A, near - E)
+        size = torch.from_numpy((want_nn(near.abs() + 1, B, ptr, False) if X is A else want_nn(A, near.abs() + 1, ptr, False))[1])
+        slope = float(((up - down) * D.double()).sum() / 2)
+        room = float((size * D.double().abs()).sum()) * (HALF[kind] + (K + 8) * 2.0 ** -24)
+        room += float((grad.cpu().double() * E.double()).abs().sum()) * (HALF[kind] + 100 * 2.0 ** -24)
+        assert abs(slope - float((grad.cpu().double() * E.double()).sum())) <= room
+
+
+def test_two_streams_and_a_captured_step(solver):
+    """Forward, both gradients and the optimiser's step as a training step uses them: on a side stream, and captured and replayed with
+    other work in between, against the same calls one after the other."""
+    import torch
+    sizes, K, width = [500, 0, 300, 77], 128, 96
+    A, B, ptr = (x.cuda() for x in draw(torch, 31, sizes, K, width, "bf16"))
+    D = torch.randn(A.shape[0], width, device="cuda").bfloat16()
+    W0 = torch.randn(len(sizes), K, width, device="cuda")
+
+    def step(W, M):
+        out = solver.op_transform_grouped(A, W.bfloat16(), ptr)
+        G = (out - D).bfloat16()
+        dA = solver.op_transform_grouped(G, W.bfloat16(), ptr, transposed=True)
+        dB = solver.op_wgrad_grouped(A, G, ptr)
+        solver.op_muon_step(W, M, dB, lr=0.02, weight_decay=0.1)
+        return out, dA, dB
+
+    W, M = W0.clone(), torch.zeros_like(W0)
+    seen = []
+    for _ in range(4):
+        out, dA, dB = step(W, M)
+        seen.append([x.clone() for x in (out, dA, dB, W, M)])
+    side = torch.cuda.Stream()
+    Ws, Ms = W0.clone(), torch.zeros_like(W0)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for k in range(4):
+            got = [*step(Ws, Ms), Ws, Ms]
+            for x, y in zip(got, seen[k]):
+                assert torch.equal(x, y)
+    torch.cuda.synchronize()
+    Wg, Mg = W0.clone(), torch.zeros_like(W0)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(Wg, Mg)
+    Wg.copy_(W0)
+    Mg.zero_()
+    for k in range(4):
+        graph.replay()
+        torch.cuda.synchronize()
+        solver.op_wgrad_grouped(A, D, ptr)                          # the program's own work in between
+        torch.cuda.synchronize()
+        for x, y in zip([*got, Wg, Mg], seen[k]):
+            assert torch.equal(x, y), k
+
+
+def test_communities_of_a_graph_are_groups(solver):
+    """comm_row_ptr of a solver's graph as the bounds, rows in the internal order."""
+    import torch
+    from paper_2112_09335_amd import binding
+    w = synth.config(1)
+    s = binding.Solver(0)
+    try:
+        s.build_graph(w.N, w.src, w.dst, w.M, w.comm)
+        g = s.get_graph()
+        ptr = torch.from_numpy(g["comm_row_ptr"])
+        A, B, _ = draw(torch, 41, np.diff(g["comm_row_ptr"]).tolist(), 40, 24, "f32")
+        out = s.op_transform_grouped(A.cuda(), B.cuda(), ptr.cuda())
+        close(out, *want_nn(A, B, ptr, False), 40, "f32")
+    finally:
+        s.close()
+
+
+def test_refusals_of_tensors(solver):
+    import torch
+    from paper_2112_09335_amd.binding import CadmmError
+    A, B, ptr = (x.cuda() for x in draw(torch, 51, [5, 6], 8, 4, "f32"))
+    bad = [
+        (A.cpu(), B, ptr), (A, B.cpu(), ptr), (A, B, ptr.cpu()), (A, B, ptr.int()), (A, B.bfloat16(), ptr), (A.double(), B.double(), ptr),
+        (A, B, ptr[:1]), (A, B[:1], ptr), (A, B[0], ptr), (A[:, :7], B, ptr), (A.T.contiguous().T, B, ptr), (A, B.transpose(1, 2), ptr),
+        (A, B, ptr.repeat(2)[::2]), (A[:1].expand(11, 8), B, ptr),
+    ]
+    for a, b, p in bad:
+        with pytest.raises(CadmmError):
+            solver.op_transform_grouped(a, b, p)
+    for out in (torch.empty(11, 5, device="cuda"), torch.empty(10, 4, device="cuda"), torch.empty(11, 4), torch.empty(11, 4, device="cuda").bfloat16()):
+        with pytest.raises(CadmmError):
+            solver.op_transform_grouped(A, B, ptr, out=out)
+    G = torch.zeros(11, 4, device="cuda")
+    for a, g, p, more in ((A, G[:10], ptr, {}), (A, G.half(), ptr, {}), (A, G, ptr[:1], {}), (A, G, ptr, dict(out_dtype=torch.float16)),
+                          (A, G, ptr, dict(out=torch.empty(2, 8, 5, device="cuda"))), (A, G, ptr, dict(out=torch.empty(2, 4, 8, device="cuda").transpose(1, 2)))):
+        with pytest.raises(CadmmError):
+            solver.op_wgrad_grouped(a, g, p, **more)
+
+
+def test_no_rows_at_all(solver):
+    import torch
+    ptr = torch.zeros(4, dtype=torch.int64, device="cuda")
+    out = solver.op_transform_grouped(torch.empty(0, 16, device="cuda"), torch.zeros(3, 16, 8, device="cuda"), ptr)
+    assert tuple(out.shape) == (0, 8)
+    dB = solver.op_wgrad_grouped(torch.empty(0, 16, device="cuda"), torch.empty(0, 8, device="cuda"), ptr)
+    assert (dB == 0).all() and tuple(dB.shape) == (3, 16, 8)

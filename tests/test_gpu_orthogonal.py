@@ -1,0 +1,224 @@
+"""GPU parity of the orthogonalised updates against the polynomial in 64 bits.
+
+Tolerances: the same products in fp32 on the CPU are off by e32 (Frobenius norm).  The kernels hold operands in 22 bits at least, where fp32
+has 24, and sum in fp32 too: 4 e32, plus 2^-20 of the result where e32 happens to be small; and the result is rounded once to
+its type."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+MUON = (3.4445, -4.7750, 2.0315)
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+
+
+@pytest.fixture(scope="module")
+def solver():
+    from paper_2112_09335_amd import binding
+    s = binding.Solver(0)
+    yield s
+    s.close()
+
+
+def types():
+    import torch
+    return {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def polynomial(G, steps, coefficients, eps):
+    """In the precision of G (numpy, batch x K x C)."""
+    a, b, c = (G.dtype.type(x) for x in coefficients)
+    out = np.empty_like(G)
+    for i, X in enumerate(G):
+        norm = np.sqrt(np.sum(X.astype(np.float64) ** 2)) + eps
+        X = (X / norm if norm > 0 else X * 0).astype(G.dtype)
+        tall = X.shape[0] > X.shape[1]
+        X = X.T if tall else X
+        for _ in range(steps):
+            S = X @ X.T
+            X = a * X + (b * S + c * (S @ S)) @ X
+        out[i] = X.T if tall else X
+    return out
+
+
+def check(got, G, kind, steps=5, coefficients=MUON, eps=1e-7):
+    """got, G: torch batch x K x C on the CPU"""
+    want = polynomial(G.double().numpy(), steps, coefficients, eps)
+    e32 = polynomial(G.float().numpy(), steps, coefficients, eps).astype(np.float64) - want
+    got = got.double().numpy()
+    assert np.isfinite(got).all()
+    for i in range(len(want)):
+        size = np.linalg.norm(want[i])
+        room = 4 * np.linalg.norm(e32[i]) + (2.0 ** -20 + HALF[kind]) * size + 1e-30
+        assert np.linalg.norm(got[i] - want[i]) <= room, (i, np.linalg.norm(got[i] - want[i]), room)
+        # entry by entry: an entry of the error before its rounding is at most the error's norm (|e_ij| <= ||e||_F)
+        most = 4 * np.linalg.norm(e32[i]) + 2.0 ** -20 * size
+        far = np.abs(got[i] - want[i])
+        assert (far <= most + HALF[kind] * (np.abs(want[i]) + most) + 2.0 ** -25).all(), (i, far.max(), most)
+
+
+def gradient(torch, seed, batch, K, width, kind, scale=1e-3):
+    rng = np.random.default_rng(seed)
+    rank = min(8, K, width)
+    strong = (rng.standard_normal((batch, K, rank)) * 0.6 ** np.arange(rank)) @ rng.standard_normal((batch, rank, width))
+    return torch.from_numpy((strong + 0.1 * rng.standard_normal((batch, K, width))) * scale).to(types()[kind])
+
+
+SHAPES = [(1, 1, 1), (1, 1, 7), (1, 5, 1), (3, 2, 2), (2, 16, 16), (1, 64, 64), (2, 33, 65), (1, 256, 64), (3, 64, 256), (1, 97, 301), (2, 128, 128),
+          (1, 130, 129), (1, 256, 256), (5, 100, 40), (1, 767, 1000), (1, 1000, 10), (2, 300, 700), (1, 512, 512), (40, 12, 20), (1, 3, 2500), (1, 640, 130),
+          (2, 192, 2048)]
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("batch,K,width", SHAPES)
+def test_orthogonalised_stack(solver, kind, batch, K, width):
+    import torch
+    G = gradient(torch, K + width, batch, K, width, kind)
+    out = solver.op_orthogonalise(G.cuda())
+    assert out.dtype == G.dtype and out.shape == G.shape
+    check(out.cpu(), G, kind)
+    assert torch.equal(out, solver.op_orthogonalise(G.cuda()))
+    if batch == 1:
+        assert torch.equal(solver.op_orthogonalise(G[0].cuda()), out[0])
+
+
+@pytest.mark.parametrize("coefficients,steps", [(MUON, 1), (MUON, 2), (MUON, 10), ((1.5, -0.5, 0.0), 12), ((15 / 8, -10 / 8, 3 / 8), 8), ((4.0, 0.0, 0.0), 4),
+                                                ((0.0, 1.0, 0.0), 1), ((-2.0, 0.5, 0.25), 3), ((0.5, 0.0, 0.0), 3)])
+@pytest.mark.parametrize("batch,K,width", [(2, 48, 80), (1, 260, 130), (1, 128, 512)])
+def test_other_polynomials(solver, coefficients, steps, batch, K, width):
+    import torch
+    G = gradient(torch, steps, batch, K, width, "f32")
+    check(solver.op_orthogonalise(G.cuda(), steps=steps, coefficients=coefficients).cpu(), G, "f32", steps, coefficients)
+
+
+def test_singular_values_come_near_one(solver):
+    """Fifteen steps of the cubic polynomial leave an orthogonal matrix: X X^T = 1 to the products' accuracy."""
+    import torch
+    rng = np.random.default_rng(5)
+    G = torch.from_numpy(rng.standard_normal((2, 60, 200))).float()
+    X = solver.op_orthogonalise(G.cuda(), steps=15, coefficients=(1.5, -0.5, 0.0), eps=0.0).cpu().double()
+    assert float((X @ X.transpose(1, 2) - torch.eye(60, dtype=torch.float64)).abs().max()) < 200 * 2.0 ** -22
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("K,width", [(30, 50), (200, 140), (256, 512)])
+def test_zeros_tiny_huge_and_not_finite(solver, kind, K, width):
+    """Matrices of a stack do not concern each other: zeros stay zeros (with eps = 0 too), sizes cancel down to the type's smallest and
+    up to its largest numbers, one entry that is no number spoils its own matrix."""
+    import torch
+    G = gradient(torch, 3, 7, K, width, "f32", 1.0)
+    G = torch.stack([G[0], G[1] * 0, G[0] * 2.0 ** -90, G[0] * 2.0 ** 118, G[4], G[5], G[0]]).to(types()[kind])
+    H = G.clone()
+    H[4, 3, 5], H[5, K - 1, 0] = float("nan"), float("inf")
+    got = solver.op_orthogonalise(H.cuda(), eps=0.0).cpu()
+    assert (got[1] == 0).all() and torch.isnan(got[4]).all() and torch.isnan(got[5]).all()
+    keep = [0, 2, 3, 6]
+    check(got[keep], G[keep], kind, eps=0.0)
+    assert torch.equal(got[0], got[6]) and torch.equal(got[0], got[2]) and torch.equal(got[0], got[3])
+    big = solver.op_orthogonalise(G.cuda(), eps=1e-7).cpu()
+    assert (big[1] == 0).all()
+    check(big[[0, 3]], G[[0, 3]], kind)
+    # far below eps: entries are held to 2^-36 of one, which five steps multiply by up to 3.4445^5 < 2^9
+    assert float((big[2].double() - torch.from_numpy(polynomial(G[2:3].double().numpy(), 5, MUON, 1e-7))[0]).abs().max()) < 2.0 ** -27
+
+
+def test_of_lower_rank_and_with_a_wide_range(solver):
+    import torch
+    rng = np.random.default_rng(9)
+    one = np.outer(rng.standard_normal(150), rng.standard_normal(90))
+    U, _ = np.linalg.qr(rng.standard_normal((150, 90)))
+    V, _ = np.linalg.qr(rng.standard_normal((90, 90)))
+    spread = U @ np.diag(10.0 ** -np.linspace(0, 6, 90)) @ V.T
+    row = np.zeros((150, 90))
+    row[7] = rng.standard_normal(90)
+    G = torch.from_numpy(np.stack([one, spread, row])).float()
+    check(solver.op_orthogonalise(G.cuda()).cpu(), G, "f32")
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("nesterov", [True, False])
+@pytest.mark.parametrize("batch,K,width", [(1, 1, 1), (3, 64, 48), (1, 97, 301), (2, 300, 200), (1, 512, 512), (2, 256, 64)])
+def test_optimiser_step(solver, kind, nesterov, batch, K, width):
+    """M in two roundings; the direction formed from it in fp32, whose roundings a matrix of full rank passes on as its own inputs' would
+    be: the direction is taken from the M that the step left."""
+    import torch
+    lr, mu, decay, scale = 0.05, 0.9, 0.1, 1.5
+    G = gradient(torch, 7, batch, K, width, kind)
+    W0 = gradient(torch, 8, batch, K, width, "f32", 0.1)
+    M0 = gradient(torch, 9, batch, K, width, "f32")
+    W, M = W0.cuda(), M0.cuda()
+    Gd = G.cuda()
+    solver.op_muon_step(W, M, Gd, lr=lr, momentum=mu, nesterov=nesterov, weight_decay=decay, scale=scale)
+    assert torch.equal(Gd.cpu(), G)
+    mu32 = float(np.float32(mu))
+    wantM = mu32 * M0.double() + G.double()
+    assert bool(((M.cpu().double() - wantM).abs() <= 2.0 ** -24 * (mu32 * M0.double().abs() + wantM.abs()) * 1.01 + 1e-44).all())
+    D = (G.double() + mu32 * M.cpu().double() if nesterov else M.cpu().double())
+    step = (W0.double() * (1 - lr * decay) - W.cpu().double()) / (lr * scale)
+    want = polynomial(D.numpy(), 5, MUON, 1e-7)
+    e32 = polynomial(D.float().numpy(), 5, MUON, 1e-7).astype(np.float64) - want
+    for i in range(batch):
+        room = 4 * np.linalg.norm(e32[i]) + 2.0 ** -20 * np.linalg.norm(want[i]) + 4 * 2.0 ** -24 * np.linalg.norm(W0[i].double().numpy()) / (lr * scale)
+        assert np.linalg.norm(step[i].numpy() - want[i]) <= room
+
+
+def test_a_step_of_a_single_matrix_and_of_a_stack_agree(solver):
+    import torch
+    G = gradient(torch, 17, 3, 70, 90, "f32").cuda()
+    W, M = torch.randn_like(G), torch.randn_like(G) * 1e-3
+    W1, M1 = W.clone(), M.clone()
+    solver.op_muon_step(W, M, G, lr=0.1)
+    for i in range(3):
+        solver.op_muon_step(W1[i], M1[i], G[i], lr=0.1)
+    assert torch.equal(W, W1) and torch.equal(M, M1)
+
+
+def test_into_its_own_input_and_from_any_element(solver):
+    import torch
+    for kind in ("f32", "bf16"):
+        G = gradient(torch, 19, 2, 65, 130, kind).cuda()
+        want = solver.op_orthogonalise(G)
+        at = torch.empty(G.numel() + 1, dtype=G.dtype, device="cuda")[1:].view(G.shape)
+        at.copy_(G)
+        out = torch.empty(G.numel() + 3, dtype=G.dtype, device="cuda")[3:].view(G.shape)
+        assert torch.equal(solver.op_orthogonalise(at, out=out), want)
+        assert torch.equal(solver.op_orthogonalise(at, out=at), want)
+
+
+def test_streams_and_captured_graphs(solver):
+    """Two captured graphs and eager calls, each with scratch of its own, replayed in turn."""
+    import torch
+    Gs = [gradient(torch, 23, 2, 200, 300, "f32").cuda(), gradient(torch, 24, 1, 256, 64, "bf16").cuda()]
+    want = [solver.op_orthogonalise(G) for G in Gs]
+    graphs, outs = [], []
+    for G in Gs:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(solver.op_orthogonalise(G))
+        graphs.append(graph)
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        for o in outs:
+            o.zero_()
+        graphs[0].replay()
+        graphs[1].replay()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            again = [solver.op_orthogonalise(G) for G in Gs]
+        torch.cuda.synchronize()
+        for o, w, x in zip(outs, want, again):
+            assert torch.equal(o, w) and torch.equal(x, w)
+
+
+def test_refusals_of_tensors(solver):
+    import torch
+    from paper_2112_09335_amd.binding import CadmmError
+    G = torch.randn(2, 8, 4, device="cuda")
+    for x, more in ((G.cpu(), {}), (G.double(), {}), (G.transpose(1, 2), {}), (G[None], {}), (G[:0], {}), (G[0, 0], {}), (G, dict(out=G[:1])),
+                    (G, dict(out=torch.empty_like(G).half())), (G, dict(steps=0)), (G, dict(eps=-1.0)), (G, dict(coefficients=(9.0, 0.0, 0.0))),
+                    (G, dict(coefficients=(1.0, 0.0)))):
+        with pytest.raises(CadmmError):
+            solver.op_orthogonalise(x, **more)
+    for W, M, x in ((G, G[:1], G), (G[0], G, G), (G.half(), G.clone(), G), (G, G.half(), G), (G, G.cpu(), G)):
+        with pytest.raises(CadmmError):
+            solver.op_muon_step(W, M, x, lr=0.1)
