@@ -3,101 +3,136 @@
 //   wgrad    : out_g  = A_g^T G_g     the sum over the rows of group g
 // Group g owns the rows [ptr[g], ptr[g+1]); the bounds are read on the device.  Whatever they hold, no row outside [0, n) is
 // touched: every bound is clamped to that range first.
+#include <algorithm>
 #include <type_traits>
 
 #include "kernels.h"
+#include "tile_product.h"
 
 namespace cadmm {
 
 namespace {
 
-template <class T> __device__ __forceinline__ float value(T x) { return (float)x; }
+using namespace tile;
 
 __device__ __forceinline__ int64_t bound_of(const int64_t* __restrict__ ptr, int g, int64_t n) {
     const int64_t p = ptr[g];
     return p < 0 ? 0 : p > n ? n : p;
 }
 
-// Rows go to workgroups in slots of BM: group g's rows [ptr[g] + i BM, ..) have slot ptr[g] / BM + g + i.  A group of len rows gets
-// at least ceil(len / BM) slots this way and at most two more than it fills, slots of different groups are apart, and the
-// group of a slot is found by a search in the bounds alone, without a prefix sum over the groups' tile counts.
-template <int BM>
-__device__ __forceinline__ int64_t first_slot(const int64_t* __restrict__ ptr, int g, int64_t n) { return bound_of(ptr, g, n) / BM + g; }
+// Rows go to workgroups in slots of `rows`: group g's rows [ptr[g] + i rows, ..) have slot ptr[g] / rows + g + i.  A group of len rows
+// gets at least ceil(len / rows) slots this way and at most two more than it fills, one at least, slots of different groups are apart,
+// and the group of a slot is found by a search in the bounds alone, without a prefix sum over the groups' tile counts.
+__device__ __forceinline__ int64_t first_slot(const int64_t* __restrict__ ptr, int g, int64_t n, int64_t rows) {
+    return bound_of(ptr, g, n) / rows + g;
+}
 // The last group whose first slot is not behind `slot`; 64 bounds are looked at in one step.
-template <int BM>
-__device__ __forceinline__ int group_of_slot(const int64_t* __restrict__ ptr, int groups, int64_t n, int64_t slot) {
+__device__ __forceinline__ int group_of_slot(const int64_t* __restrict__ ptr, int groups, int64_t n, int64_t rows, int64_t slot) {
     const int lane = threadIdx.x & 63;
     int at = 0, left = groups;                         // the answer is in [at, at + left)
     while (left > 1) {
         const int stride = (left + 63) / 64;
         const int g = lane * stride;
-        const bool in = g < left && first_slot<BM>(ptr, at + g, n) <= slot;
+        const bool in = g < left && first_slot(ptr, at + g, n, rows) <= slot;
         const int found = __popcll(__ballot(in));      // (the bounds do not descend: the lanes that are in come first)
         const int skip = (found > 0 ? found - 1 : 0) * stride;
         at += skip;
         left = left - skip < stride ? left - skip : stride;
     }
-    return at;
+    return __builtin_amdgcn_readfirstlane(at);
 }
 
-constexpr int ST = 64, SK = 16;        // results of a workgroup in each direction, and of the contraction per step
+// Workgroup -> (slot, tile).  Consecutive workgroups go round-robin to the eight XCDs, each with an L2 of its own.  In slices, every
+// XCD walks one contiguous part of the list, tiles of a slot one after the other and slots of a group too, so that what they share comes
+// from its L2.  With few rows a group the slots that hold rows are not spread evenly over the list, and plain order is kept.
+__device__ __forceinline__ void place(unsigned tiles, bool slices, int64_t& slot, int& t) {
+    unsigned b = blockIdx.x;
+    if (slices) {
+        const unsigned nb = gridDim.x, each = nb / 8, whole = each * 8;
+        if (b < whole) b = (b & 7u) * each + (b >> 3);
+    }
+    slot = b / tiles;
+    t = (int)(b % tiles);
+}
 
-// 64 x 64 results on the vector ALU in fp32: X(i, k) at X + i xi + k xk, Y(k, j) at Y + k yk + j yj.
-template <class T>
-__device__ __forceinline__ void simple_tile(float (&acc)[4][4], const T* __restrict__ X, int64_t xi, int64_t xk, const T* __restrict__ Y,
-                                            int64_t yk, int64_t yj, int64_t rows, int64_t cols, int64_t depth) {
-    __shared__ float Xs[SK][ST + 4], Ys[SK][ST + 4];
-    const int tid = threadIdx.x, ti = tid >> 4, tj = tid & 15;
-    for (int64_t k0 = 0; k0 < depth; k0 += SK) {
-        __syncthreads();
-        for (int f = tid; f < SK * ST; f += 256) {
-            const int i = f / SK, k = f % SK;
-            Xs[k][i] = i < rows && k0 + k < depth ? value(X[i * xi + (k0 + k) * xk]) : 0.f;
-            Ys[k][i] = i < cols && k0 + k < depth ? value(Y[(k0 + k) * yk + i * yj]) : 0.f;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < SK; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] += Xs[k][ti * 4 + i] * Ys[k][tj * 4 + j];
+template <class P, class T, Lie YL>
+__global__ __launch_bounds__(P::THREADS, P::THREADS == 256 ? 2 : 1) void grouped_nn_kernel(
+    const T* __restrict__ A, int64_t n, int64_t lda, int K, const T* __restrict__ B, int C, int groups, const int64_t* __restrict__ ptr,
+    T* __restrict__ out, int64_t ldo, int col_tiles, int slices, int whole_out) {
+    __shared__ __align__(16) unsigned short S[P::kLds];
+    int64_t slot;
+    int tile;
+    place(col_tiles, slices, slot, tile);
+    const int g = group_of_slot(ptr, groups, n, P::BM, slot);
+    const int64_t skip = slot - first_slot(ptr, g, n, P::BM);
+    const int64_t r0 = bound_of(ptr, g, n) + skip * P::BM, end = bound_of(ptr, g + 1, n);
+    if (skip < 0 || r0 >= end) return;
+    const int c0 = tile * P::BN, rows = end - r0 < P::BM ? (int)(end - r0) : P::BM;
+    const T* Bg = B + (int64_t)g * K * C;
+    floatx16 acc[P::TM][P::TN];
+    const View<T> x{A + r0 * lda, lda, rows, K, 0};
+    const View<T> y = YL == kAlong ? View<T>{Bg + (int64_t)c0 * K, K, C - c0, K, 0} : View<T>{Bg + c0, C, C - c0, K, 0};
+    P::run(acc, x, y, S);
+    P::drain(acc, S, [&](int row, int col, float4 v) {
+        if (row < rows && c0 + col < C) put(out + (r0 + row) * ldo, c0 + col, C, v, whole_out);
+    });
+}
+
+// Rows of a group beyond `most` go to further workgroups of their own, whose sums are added by grouped_tn_reduce_kernel: the i-th such
+// part of group g is number 2 (ptr[g] / most + i) (+ 1 unless it is the group's last) of `partial`.  (Groups in parts have more than
+// `most` rows: no two parts that begin in the same stretch of `most` rows are both last or both not.)
+__device__ __forceinline__ int64_t part_place(int64_t lo, int64_t hi, int64_t most, int64_t i) {
+    return 2 * (lo / most + i) + (lo + (i + 1) * most < hi ? 1 : 0);
+}
+
+template <class P, class T, class O>
+__global__ __launch_bounds__(P::THREADS, P::THREADS == 256 ? 2 : 1) void grouped_tn_kernel(
+    const T* __restrict__ A, int64_t n, int64_t lda, int K, const T* __restrict__ G, int64_t ldg, int C, int groups,
+    const int64_t* __restrict__ ptr, O* __restrict__ out, float* __restrict__ partial, int64_t most, int64_t part_size, int col_tiles, int tiles,
+    int slices, int whole_out) {
+    __shared__ __align__(16) unsigned short S[P::kLds];
+    int64_t slot;
+    int tile;
+    place(tiles, slices, slot, tile);
+    const int g = group_of_slot(ptr, groups, n, most, slot);
+    const int64_t lo = bound_of(ptr, g, n), end = bound_of(ptr, g + 1, n), hi = end > lo ? end : lo;
+    const int64_t i = slot - first_slot(ptr, g, n, most), r0 = lo + i * most;
+    if (i < 0 || (i > 0 && r0 >= hi)) return;
+    const int i0 = tile / col_tiles * P::BM, c0 = tile % col_tiles * P::BN;
+    floatx16 acc[P::TM][P::TN];
+    const int64_t depth = hi - r0 < most ? hi - r0 : most;
+    P::run(acc, View<T>{A + r0 * lda + i0, lda, K - i0, depth, 0}, View<T>{G + r0 * ldg + c0, ldg, C - c0, depth, 0}, S);
+    if (hi - lo > most) {
+        float* to = partial + part_place(lo, hi, most, i) * part_size;
+        P::drain(acc, S, [&](int row, int col, float4 v) {
+            if (i0 + row < K && c0 + col < C) put(to + (int64_t)(i0 + row) * C, c0 + col, C, v, whole_out);
+        });
+    } else {
+        O* to = out + (int64_t)g * K * C;
+        P::drain(acc, S, [&](int row, int col, float4 v) {
+            if (i0 + row < K && c0 + col < C) put(to + (int64_t)(i0 + row) * C, c0 + col, C, v, whole_out);
+        });
     }
 }
+
 template <class O>
-__device__ __forceinline__ void simple_store(const float (&acc)[4][4], O* __restrict__ out, int64_t ld, int64_t rows, int64_t cols) {
-    const int ti = threadIdx.x >> 4, tj = threadIdx.x & 15;
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j)
-            if (ti * 4 + i < rows && tj * 4 + j < cols) out[(ti * 4 + i) * ld + tj * 4 + j] = (O)acc[i][j];
-}
-
-template <class T>
-__global__ __launch_bounds__(256) void grouped_nn_kernel(const T* __restrict__ A, int64_t n, int64_t lda, int K, const T* __restrict__ B,
-                                                         int C, int transposed, int groups, const int64_t* __restrict__ ptr,
-                                                         T* __restrict__ out, int64_t ldo, int col_tiles) {
-    const int64_t slot = blockIdx.x / col_tiles;
-    const int c0 = (int)(blockIdx.x % col_tiles) * ST;
-    const int g = group_of_slot<ST>(ptr, groups, n, slot);
-    const int64_t skip = slot - first_slot<ST>(ptr, g, n);
-    const int64_t r0 = bound_of(ptr, g, n) + skip * ST, end = bound_of(ptr, g + 1, n);
-    if (skip < 0 || r0 >= end) return;
-    float acc[4][4] = {};
-    const T* Bg = B + (int64_t)g * K * C + (transposed ? (int64_t)c0 * K : c0);
-    simple_tile(acc, A + r0 * lda, lda, 1, Bg, transposed ? 1 : C, transposed ? K : 1, end - r0, C - c0, K);
-    simple_store(acc, out + r0 * ldo + c0, ldo, end - r0, C - c0);
-}
-
-template <class T, class O>
-__global__ __launch_bounds__(256) void grouped_tn_kernel(const T* __restrict__ A, int64_t n, int64_t lda, int K, const T* __restrict__ G,
-                                                         int64_t ldg, int C, const int64_t* __restrict__ ptr, O* __restrict__ out,
-                                                         int col_tiles, int tiles) {
-    const int g = (int)(blockIdx.x / tiles), t = (int)(blockIdx.x % tiles);
-    const int i0 = t / col_tiles * ST, c0 = t % col_tiles * ST;
+__global__ __launch_bounds__(256) void grouped_tn_reduce_kernel(const float* __restrict__ partial, int64_t n, const int64_t* __restrict__ ptr, int64_t most,
+                                                                int64_t part_size, int64_t count, O* __restrict__ out) {
+    const int g = blockIdx.y;
     const int64_t lo = bound_of(ptr, g, n), hi = bound_of(ptr, g + 1, n);
-    float acc[4][4] = {};
-    simple_tile(acc, A + lo * lda + i0, 1, lda, G + lo * ldg + c0, ldg, 1, K - i0, C - c0, hi - lo);
-    simple_store(acc, out + ((int64_t)g * K + i0) * C + c0, C, K - i0, C - c0);
+    if (hi - lo <= most) return;
+    const int64_t parts = (hi - lo + most - 1) / most;
+    for (int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; e < count; e += (int64_t)gridDim.x * 1024) {
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int64_t i = 0; i < parts; ++i) {
+            const float4 v = *reinterpret_cast<const float4*>(partial + part_place(lo, hi, most, i) * part_size + e);      // (parts are padded to fours)
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+        const float w[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (e + k < count) out[(int64_t)g * count + e + k] = (O)w[k];
+    }
 }
 
 template <class F>
@@ -107,33 +142,129 @@ void with_type(int type, F f) {
     else f((float*)nullptr);
 }
 
+// Tiles (wavefronts, 32 x 32 accumulators of one, contraction per step, steps ahead).  Large ones read each operand from LDS once for
+// 128 x 256 results, two workgroups a compute unit; the small ones are for products that would not fill the chip with them.
+template <class T> constexpr int kStep = sizeof(T) == 4 ? 16 : 32;
+template <class T, Lie X, Lie Y, Mode M> using Large = Product<T, X, Y, M, 2, 2, 2, 4, kStep<T>, 1>;          // 128 x 256
+template <class T, Lie X, Lie Y, Mode M> using Middle = Product<T, X, Y, M, 2, 2, 2, 2, kStep<T>, 2>;         // 128 x 128
+template <class T, Lie X, Lie Y, Mode M> using Small = Product<T, X, Y, M, 2, 2, 1, 1, 2 * kStep<T>, 2>;      // 64 x 64
+template <class T, Lie X, Lie Y, Mode M> using Few = Product<T, X, Y, M, 1, 2, 1, 1, 2 * kStep<T>, 4>;        // 32 x 64
+
+enum Size { kLarge, kMiddle, kSmall, kFew };
+constexpr int kSizeRows[] = {128, 128, 64, 32}, kSizeCols[] = {256, 128, 64, 64};
+constexpr int64_t kCus = 256;
+
+int64_t over(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+Size nn_size(int64_t n, int C, int groups) {
+    const int64_t hit = std::min<int64_t>(n, groups), rows = over(n, hit);            // rows of a group that has any, if they share alike
+    for (Size s : {kLarge, kMiddle, kSmall}) {
+        const bool fits = C > kSizeCols[s] / 2 && rows > kSizeRows[s] / 2;
+        if (fits && (n / kSizeRows[s] + hit / 2) * over(C, kSizeCols[s]) >= kCus) return s;
+    }
+    return rows > 32 ? kSmall : kFew;
+}
+
+struct TnPlan { Size size; int64_t most, parts; };
+TnPlan tn_plan(int64_t n, int K, int C, int groups) {
+    const Size s = K > 64 && C > 128 ? kLarge : K > 64 && C > 64 ? kMiddle : kSmall;
+    const int64_t tiles = over(K, kSizeRows[s]) * over(C, kSizeCols[s]);
+    TnPlan p{s, n > 0 ? n : 1, 0};
+    // too few tiles for two workgroups a compute unit: the rows are shared out too, 256 of them at least
+    if (tiles * groups < 2 * kCus * 2) p.most = std::max<int64_t>(256, over(over(n * tiles, 2 * kCus), 64) * 64);
+    p.parts = p.most < n ? 2 * (n / p.most + 1) : 0;
+    return p;
+}
+int64_t part_floats(int K, int C) { return over((int64_t)K * C, 4) * 4; }
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+template <Size SIZE, class T, Lie X, Lie Y, Mode M>
+using Sized = std::conditional_t<SIZE == kLarge, Large<T, X, Y, M>, std::conditional_t<SIZE == kMiddle, Middle<T, X, Y, M>,
+              std::conditional_t<SIZE == kSmall, Small<T, X, Y, M>, Few<T, X, Y, M>>>>;
+
+template <class T, Lie YL, Mode MODE>
+void nn_launch(hipStream_t s, const GroupedNN& a, Size size, bool whole_out) {
+    auto go = [&](auto sized) {
+        using P = Sized<decltype(sized)::value, T, kAlong, YL, MODE>;
+        const int col_tiles = (int)over(a.C, P::BN);
+        const int64_t blocks = (a.n / P::BM + a.groups) * col_tiles;
+        grouped_nn_kernel<P, T, YL><<<dim3((unsigned)blocks), dim3(P::THREADS), 0, s>>>(
+            (const T*)a.A, a.n, a.lda, a.K, (const T*)a.B, a.C, a.groups, a.ptr, (T*)a.out, a.ldo, col_tiles, a.n / P::BM >= a.groups, whole_out);
+    };
+    if (size == kLarge) go(std::integral_constant<Size, kLarge>());
+    else if (size == kMiddle) go(std::integral_constant<Size, kMiddle>());
+    else if (size == kSmall) go(std::integral_constant<Size, kSmall>());
+    else go(std::integral_constant<Size, kFew>());
+}
+
+template <class T, Mode MODE, class O>
+void tn_launch(hipStream_t s, const GroupedTN& a, const TnPlan& plan) {
+    float* partial = (float*)a.scratch;
+    const int64_t count = (int64_t)a.K * a.C;
+    auto go = [&](auto sized) {
+        using P = Sized<decltype(sized)::value, T, kAcross, kAcross, MODE>;
+        const int col_tiles = (int)over(a.C, P::BN), tiles = col_tiles * (int)over(a.K, P::BM);
+        const int64_t blocks = (a.n / plan.most + a.groups) * tiles;
+        grouped_tn_kernel<P, T, O><<<dim3((unsigned)blocks), dim3(P::THREADS), 0, s>>>(
+            (const T*)a.A, a.n, a.lda, a.K, (const T*)a.G, a.ldg, a.C, a.groups, a.ptr, (O*)a.out, partial, plan.most, part_floats(a.K, a.C), col_tiles,
+            tiles, a.n / plan.most >= a.groups, a.C % 4 == 0 && ((uintptr_t)a.out & (4 * sizeof(O) - 1)) == 0);
+    };
+    if (plan.size == kLarge) go(std::integral_constant<Size, kLarge>());
+    else if (plan.size == kMiddle) go(std::integral_constant<Size, kMiddle>());
+    else go(std::integral_constant<Size, kSmall>());
+    if (plan.parts > 0) {
+        const unsigned bx = (unsigned)std::min<int64_t>(over(count, 1024), std::max<int64_t>(1, 8 * kCus / a.groups));
+        for (int g0 = 0; g0 < a.groups; g0 += 65535)       // (a grid's second dimension)
+            grouped_tn_reduce_kernel<O><<<dim3(bx, (unsigned)std::min(a.groups - g0, 65535)), dim3(256), 0, s>>>(
+                partial, a.n, a.ptr + g0, plan.most, part_floats(a.K, a.C), count, (O*)a.out + (int64_t)g0 * count);
+    }
+}
+
 }  // namespace
 
-int64_t grouped_nn_blocks(int64_t n, int C, int groups) { return (n / ST + groups) * ((C + ST - 1) / ST); }
-int64_t grouped_tn_blocks(int64_t, int K, int C, int groups) { return (int64_t)groups * ((K + ST - 1) / ST) * ((C + ST - 1) / ST); }
-size_t grouped_tn_scratch(int64_t, int, int, int) { return 0; }
+int64_t grouped_nn_blocks(int64_t n, int C, int groups) {
+    if (n == 0) return 0;
+    const Size s = nn_size(n, C, groups);
+    return (n / kSizeRows[s] + groups) * over(C, kSizeCols[s]);
+}
+int64_t grouped_tn_blocks(int64_t n, int K, int C, int groups) {
+    const TnPlan p = tn_plan(n, K, C, groups);
+    return (n / p.most + groups) * over(K, kSizeRows[p.size]) * over(C, kSizeCols[p.size]);
+}
+size_t grouped_tn_scratch(int64_t n, int K, int C, int groups) { return sizeof(float) * tn_plan(n, K, C, groups).parts * part_floats(K, C); }
 
 void launch_grouped_nn(hipStream_t s, int type, const GroupedNN& a) {
-    const int col_tiles = (a.C + ST - 1) / ST;
     if (a.n == 0) return;
+    const Size size = nn_size(a.n, a.C, a.groups);
     with_type(type, [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        grouped_nn_kernel<T><<<dim3((unsigned)grouped_nn_blocks(a.n, a.C, a.groups)), dim3(256), 0, s>>>(
-            (const T*)a.A, a.n, a.lda, a.K, (const T*)a.B, a.C, a.transposed, a.groups, a.ptr, (T*)a.out, a.ldo, col_tiles);
+        constexpr int64_t Q = 16 / sizeof(T);
+        const bool whole = a.K % 8 == 0 && a.lda % Q == 0 && aligned16(a.A) && aligned16(a.B) && (a.transposed || a.C % 8 == 0);
+        const bool whole_out = a.C % 4 == 0 && a.ldo % 4 == 0 && ((uintptr_t)a.out & (4 * sizeof(T) - 1)) == 0;
+        if (a.transposed) {
+            if (whole) nn_launch<T, kAlong, kWhole>(s, a, size, whole_out);
+            else nn_launch<T, kAlong, kAny>(s, a, size, whole_out);
+        } else {
+            if (whole) nn_launch<T, kAcross, kWhole>(s, a, size, whole_out);
+            else nn_launch<T, kAcross, kAny>(s, a, size, whole_out);
+        }
     });
 }
 
 void launch_grouped_tn(hipStream_t s, int type, int out_type, const GroupedTN& a) {
-    const int col_tiles = (a.C + ST - 1) / ST, tiles = col_tiles * ((a.K + ST - 1) / ST);
+    const TnPlan plan = tn_plan(a.n, a.K, a.C, a.groups);
     with_type(type, [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        const dim3 grid((unsigned)grouped_tn_blocks(a.n, a.K, a.C, a.groups));
-        if (out_type == kF32)
-            grouped_tn_kernel<T, float><<<grid, dim3(256), 0, s>>>((const T*)a.A, a.n, a.lda, a.K, (const T*)a.G, a.ldg, a.C, a.ptr,
-                                                                   (float*)a.out, col_tiles, tiles);
-        else
-            grouped_tn_kernel<T, T><<<grid, dim3(256), 0, s>>>((const T*)a.A, a.n, a.lda, a.K, (const T*)a.G, a.ldg, a.C, a.ptr, (T*)a.out,
-                                                               col_tiles, tiles);
+        constexpr int64_t Q = 16 / sizeof(T);
+        const bool whole = a.K % 8 == 0 && a.C % 8 == 0 && a.lda % Q == 0 && a.ldg % Q == 0 && aligned16(a.A) && aligned16(a.G);
+        auto go = [&](auto* o) {
+            using O = std::remove_pointer_t<decltype(o)>;
+            if (whole) tn_launch<T, kWhole, O>(s, a, plan);
+            else tn_launch<T, kAny, O>(s, a, plan);
+        };
+        if (out_type == kF32) go((float*)nullptr);
+        else go((T*)nullptr);
     });
 }
 
