@@ -1,98 +1,234 @@
 // Updates with their singular values brought towards one: X <- a X + (b S + c S^2) X with S = X X^T, an odd polynomial of the
 // matrix that leaves its singular vectors alone and takes every singular value x to a x + b x^3 + c x^5, applied a few times to
-// every matrix of a stack over its Frobenius norm.  S is formed on the smaller side: r = min(K, C) rows of s = max(K, C).
+// every matrix of a stack over its Frobenius norm.  With K <= C, S = X X^T and X <- P X for P = a + b S + c S^2; else S = X^T X and
+// X <- X P: no matrix is transposed, the operands lie along or across the contraction as it comes (tile_product.h).
+//
+// Between the launches X, S and P are kept as pairs of fp16 (22 bits), each scaled by a power of two that keeps its largest possible
+// entry below 2^15: a singular value of X is bounded by what the polynomial makes of [0, 1] (polynomial_bound), an entry by the
+// largest singular value.  What a pair drops is below 2^-38 of that bound, or 2^-23 of the entry.  The polynomial multiplies small
+// singular values by a (3.4445) a step, errors with them: sixteen bits or less would show in a result of bf16.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
 
 #include "kernels.h"
+#include "tile_product.h"
 
 namespace cadmm {
 
 namespace {
 
-constexpr int ST = 64, SK = 16;
+using namespace tile;
 
-// One workgroup a matrix: the direction D (G itself, or what the momentum makes of it) and its norm, then X = D / (norm + eps), tall
-// matrices transposed.
+constexpr int kNormBlocks = 64;        // most workgroups that add up one matrix's norm
+
+// The direction of the update: the gradient, or what the momentum makes of it.
 template <class T>
-__global__ __launch_bounds__(256) void orthogonal_begin_kernel(const T* __restrict__ G, float* __restrict__ M, float mu, int nesterov, int K,
-                                                               int C, float eps, float* __restrict__ X) {
-    const int64_t count = (int64_t)K * C, base = blockIdx.x * count;
-    __shared__ double sums[256];
+struct Source {
+    const T* G; float* M; float mu; int nesterov;
+    __device__ __forceinline__ float first(int64_t e) const {             // with the momentum brought forward
+        const float g = (float)G[e];
+        if (!M) return g;
+        const float m = mu * M[e] + g;
+        M[e] = m;
+        return nesterov ? g + mu * m : m;
+    }
+    __device__ __forceinline__ float again(int64_t e) const {
+        if (!M) return (float)G[e];
+        const float m = M[e];
+        return nesterov ? (float)G[e] + mu * m : m;
+    }
+};
+
+template <class T>
+__global__ __launch_bounds__(256) void orthogonal_norm_kernel(Source<T> src, int64_t count, double* __restrict__ norms) {
+    const int64_t base = blockIdx.y * count;
+    __shared__ double sums[4];
     double sum = 0.0;
-    for (int64_t f = threadIdx.x; f < count; f += 256) {
-        float d = (float)G[base + f];
-        if (M) {
-            const float m = mu * M[base + f] + d;
-            M[base + f] = m;
-            d = nesterov ? d + mu * m : m;
-        }
-        X[base + (K > C ? f % C * K + f / C : f)] = d;
-        sum += (double)d * (double)d;
+    for (int64_t f = (int64_t)blockIdx.x * 256 + threadIdx.x; f < count; f += (int64_t)gridDim.x * 256) {
+        const double d = src.first(base + f);
+        sum += d * d;
     }
-    sums[threadIdx.x] = sum;
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
     __syncthreads();
-    for (int o = 128; o > 0; o >>= 1) {
-        if ((int)threadIdx.x < o) sums[threadIdx.x] += sums[threadIdx.x + o];
-        __syncthreads();
-    }
-    const double norm = sqrt(sums[0]) + (double)eps, inv = norm > 0.0 ? 1.0 / norm : norm == 0.0 ? 0.0 : norm;
-    for (int64_t f = threadIdx.x; f < count; f += 256) X[base + f] = (float)((double)X[base + f] * inv);
+    if (threadIdx.x == 0) norms[blockIdx.y * kNormBlocks + blockIdx.x] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
 }
 
-// out = alpha D + beta L R for every matrix of the stack (D may be null); L m x k, R k x p, or with RT its transpose p x k.
-template <bool RT>
-__global__ __launch_bounds__(256) void orthogonal_product_kernel(const float* __restrict__ L, const float* __restrict__ R, const float* __restrict__ D,
-                                                                 float* __restrict__ out, int m, int k, int p, float alpha, float beta) {
-    const int64_t b = blockIdx.z;
-    const int i0 = blockIdx.y * ST, j0 = blockIdx.x * ST;
-    L += b * m * k; R += b * k * p; out += b * m * p;
-    __shared__ float Ls[SK][ST + 4], Rs[SK][ST + 4];
-    const int tid = threadIdx.x, ti = tid >> 4, tj = tid & 15;
-    float acc[4][4] = {}, sum[4][4] = {};
-    // (sums of 128 products are added up: a single chain of thousands would cost three bits)
-    auto gather = [&] {
-        for (int i = 0; i < 4; ++i)
-            for (int j = 0; j < 4; ++j) { sum[i][j] += acc[i][j]; acc[i][j] = 0.f; }
-    };
-    for (int k0 = 0; k0 < k; k0 += SK) {
-        if (k0 % 128 == 0) gather();
-        __syncthreads();
-        for (int f = tid; f < SK * ST; f += 256) {
-            const int i = f / SK, kk = f % SK;
-            const int row = i0 + i, col = j0 + i, at = k0 + kk;
-            Ls[kk][i] = row < m && at < k ? L[(int64_t)row * k + at] : 0.f;
-            Rs[kk][i] = col < p && at < k ? RT ? R[(int64_t)col * k + at] : R[(int64_t)at * p + col] : 0.f;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int kk = 0; kk < SK; ++kk)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] += Ls[kk][ti * 4 + i] * Rs[kk][tj * 4 + j];
-    }
-    gather();
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const int row = i0 + ti * 4 + i, col = j0 + tj * 4 + j;
-            if (row >= m || col >= p) continue;
-            const int64_t o = (int64_t)row * p + col;
-            out[o] = D ? alpha * D[b * m * p + o] + beta * sum[i][j] : beta * sum[i][j];
-        }
+__device__ __forceinline__ void split_pair(float x, _Float16& h, _Float16& l) {
+    h = (_Float16)x;
+    l = (_Float16)(x - (float)h);
+}
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void put_pair(_Float16* to, int64_t plane, float4 v) {
+    f16x4 h, l;
+    _Float16 a, b;
+    split_pair(v.x, a, b); h.x = a; l.x = b;
+    split_pair(v.y, a, b); h.y = a; l.y = b;
+    split_pair(v.z, a, b); h.z = a; l.z = b;
+    split_pair(v.w, a, b); h.w = a; l.w = b;
+    *reinterpret_cast<f16x4*>(to) = h;
+    *reinterpret_cast<f16x4*>(to + plane) = l;
 }
 
+// X = direction / (norm + eps), scaled, as pairs; rows of ld elements, what is past a row's end is zero.
 template <class T>
-__global__ __launch_bounds__(256) void orthogonal_end_kernel(const float* __restrict__ X, int K, int C, T* __restrict__ out, float* __restrict__ W,
-                                                             float keep, float rate) {
-    const int64_t count = (int64_t)K * C, base = blockIdx.y * count;
-    for (int64_t f = blockIdx.x * 256 + threadIdx.x; f < count; f += (int64_t)gridDim.x * 256) {
-        const float x = X[base + (K > C ? f % C * K + f / C : f)];
-        if (W) W[base + f] = keep * W[base + f] - rate * x;
-        else out[base + f] = (T)x;
+__global__ __launch_bounds__(256) void orthogonal_begin_kernel(Source<T> src, const double* __restrict__ norms, int n_norms, int K, int C, int ld,
+                                                               float eps, float scale, _Float16* __restrict__ X, int64_t plane) {
+    const int64_t b = blockIdx.y;
+    double sum = 0.0;
+    for (int i = 0; i < n_norms; ++i) sum += norms[b * kNormBlocks + i];
+    const double norm = sqrt(sum) + (double)eps;
+    // (no direction: zero; an entry that is not finite: nothing is)
+    const double inv = norm == 0.0 ? 0.0 : norm < HUGE_VAL ? (double)scale / norm : __builtin_nan("");
+    const int quads = ld / 4;
+    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < (int64_t)K * quads; q += (int64_t)gridDim.x * 256) {
+        const int64_t row = q / quads;
+        const int c = (int)(q % quads) * 4;
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = c + e < C ? (float)((double)src.again(b * K * C + row * C + c + e) * inv) : 0.f;
+        put_pair(X + (b * K + row) * ld + c, plane, make_float4(v[0], v[1], v[2], v[3]));
     }
 }
+
+struct Stack {                          // pairs: matrices of rows x ld
+    _Float16* p; int64_t plane, each; int ld;
+    __device__ __forceinline__ View<Pair> view(int64_t b, int64_t at, int rows, int64_t depth) const { return {p + b * each + at, ld, rows, depth, plane}; }
+};
+
+// Workgroup -> (matrix, tile row, tile column); tiles of a matrix one after the other on one XCD (see the products over groups).
+__device__ __forceinline__ void place(int tile_rows, int tile_cols, int64_t& b, int& ti, int& tj) {
+    unsigned at = blockIdx.x;
+    const unsigned each = gridDim.x / 8, whole = each * 8;
+    if (at < whole) at = (at & 7u) * each + (at >> 3);
+    const unsigned tiles = (unsigned)tile_rows * tile_cols;
+    b = at / tiles;
+    ti = (int)(at % tiles) / tile_cols;
+    tj = (int)(at % tiles) % tile_cols;
+}
+
+// out = alpha X^T X or X X^T (LIE: kAlong forms X X^T), or with `from` = X symmetric: alpha X X + beta X + gamma 1.  The result is symmetric:
+// tiles below the diagonal are left out, and of the others every entry on or above it is stored to both its places.
+template <class P, Lie LIE>
+__global__ __launch_bounds__(P::THREADS, 2) void orthogonal_square_kernel(Stack x, int r, int64_t depth, Stack out, float alpha, float beta, float gamma,
+                                                                          int with_linear, int tile_rows, int tile_cols) {
+    __shared__ __align__(16) unsigned short S[P::kLds];
+    int64_t b;
+    int ti, tj;
+    place(tile_rows, tile_cols, b, ti, tj);
+    const int i0 = ti * P::BM, c0 = tj * P::BN;
+    if (i0 >= c0 + P::BN) return;
+    floatx16 acc[P::TM][P::TN];
+    if (LIE == kAlong) P::run(acc, x.view(b, (int64_t)i0 * x.ld, r - i0, depth), x.view(b, (int64_t)c0 * x.ld, r - c0, depth), S);
+    else P::run(acc, x.view(b, i0, x.ld - i0, depth), x.view(b, c0, x.ld - c0, depth), S);
+    _Float16* to = out.p + b * out.each;
+    const _Float16* lin = x.p + b * x.each;
+    const bool crossing = c0 < i0 + P::BM;                 // the tile holds entries below the diagonal
+    auto own = [&](int row, int col, float4 v) {
+        const int i = i0 + row, j = c0 + col;
+        float w[4] = {alpha * v.x, alpha * v.y, alpha * v.z, alpha * v.w};
+        if (i >= r || j >= out.ld) return v;
+        if (with_linear) {
+            const f16x4 h = *reinterpret_cast<const f16x4*>(lin + (int64_t)i * x.ld + j), l = *reinterpret_cast<const f16x4*>(lin + (int64_t)i * x.ld + j + x.plane);
+            const float s[4] = {(float)h.x + (float)l.x, (float)h.y + (float)l.y, (float)h.z + (float)l.z, (float)h.w + (float)l.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = w[e] + beta * s[e] + (j + e == i ? gamma : 0.f);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = j + e < r ? w[e] : 0.f;
+        const float4 q = make_float4(w[0], w[1], w[2], w[3]);
+        _Float16* at = to + (int64_t)i * out.ld + j;
+        if (!crossing || j >= i) put_pair(at, out.plane, q);
+        else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (j + e >= i) split_pair(w[e], at[e], at[e + out.plane]);
+        }
+        return q;
+    };
+    // (rows r .. ld of the result are never read; columns r .. ld hold zeros, which the own side of the last tile column leaves)
+    auto mirror = [&](int col, int row, float4 v) {
+        const int i = i0 + row, j = c0 + col;
+        if (j >= r || i >= r) return;
+        const float w[4] = {v.x, v.y, v.z, v.w};
+        _Float16* at = to + (int64_t)j * out.ld + i;
+        if (i + 3 < j) put_pair(at, out.plane, v);
+        else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (i + e < j) split_pair(w[e], at[e], at[e + out.plane]);
+        }
+    };
+    P::template drain<true>(acc, S, own, mirror);
+}
+
+// X <- P X (YL: X lies across the contraction) or X P (P is symmetric and lies along it), alpha times; the last time to `out` or off W.
+template <class O> struct Target { O* out; float* W; float keep, rate; };
+template <class P, Lie YL, class O>
+__global__ __launch_bounds__(P::THREADS, 2) void orthogonal_apply_kernel(Stack left, Stack right, int K, int C, int r, Stack next, Target<O> last, float alpha,
+                                                                         int tile_rows, int tile_cols) {
+    __shared__ __align__(16) unsigned short S[P::kLds];
+    int64_t b;
+    int ti, tj;
+    place(tile_rows, tile_cols, b, ti, tj);
+    const int i0 = ti * P::BM, c0 = tj * P::BN;
+    floatx16 acc[P::TM][P::TN];
+    P::run(acc, left.view(b, (int64_t)i0 * left.ld, K - i0, r), YL == kAcross ? right.view(b, c0, right.ld - c0, r) : right.view(b, (int64_t)c0 * right.ld, C - c0, r), S);
+    if (next.p) {
+        _Float16* to = next.p + b * next.each;
+        P::drain(acc, S, [&](int row, int col, float4 v) {
+            const int i = i0 + row, j = c0 + col;
+            if (i >= K || j >= next.ld) return;
+            put_pair(to + (int64_t)i * next.ld + j, next.plane,
+                     make_float4(j < C ? alpha * v.x : 0.f, j + 1 < C ? alpha * v.y : 0.f, j + 2 < C ? alpha * v.z : 0.f, j + 3 < C ? alpha * v.w : 0.f));
+        });
+    } else if (last.W) {
+        float* W = last.W + b * K * C;
+        P::drain(acc, S, [&](int row, int col, float4 v) {
+            const int i = i0 + row, j = c0 + col;
+            if (i >= K) return;
+            const float w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (j + e < C) W[(int64_t)i * C + j + e] = last.keep * W[(int64_t)i * C + j + e] - last.rate * (alpha * w[e]);
+        });
+    } else {
+        O* to = last.out + b * K * C;
+        const bool whole = C % 4 == 0 && (reinterpret_cast<uintptr_t>(to) & (4 * sizeof(O) - 1)) == 0;
+        P::drain(acc, S, [&](int row, int col, float4 v) {
+            const int i = i0 + row, j = c0 + col;
+            if (i < K && j < C) put(to + (int64_t)i * C, j, C, make_float4(alpha * v.x, alpha * v.y, alpha * v.z, alpha * v.w), whole);
+        });
+    }
+}
+
+template <Lie X, Lie Y> using Large = Product<Pair, X, Y, kWhole, 2, 2, 2, 4, 16, 1>;      // 128 x 256
+template <Lie X, Lie Y> using Middle = Product<Pair, X, Y, kWhole, 2, 2, 2, 2, 16, 2>;     // 128 x 128
+template <Lie X, Lie Y> using Small = Product<Pair, X, Y, kWhole, 2, 2, 1, 1, 32, 2>;      // 64 x 64
+enum Size { kLarge, kMiddle, kSmall };
+constexpr int kSizeRows[] = {128, 128, 64}, kSizeCols[] = {256, 128, 64};
+template <Size SIZE, Lie X, Lie Y>
+using Sized = std::conditional_t<SIZE == kLarge, Large<X, Y>, std::conditional_t<SIZE == kMiddle, Middle<X, Y>, Small<X, Y>>>;
+
+int64_t over(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int64_t round8(int64_t n) { return (n + 7) / 8 * 8; }
+constexpr int64_t kCus = 256;
+// The largest tiles that give every compute unit one; half: of a symmetric result only that much is formed.
+Size size_of(int64_t batch, int64_t rows, int64_t cols, bool half) {
+    for (Size s : {kLarge, kMiddle})
+        if (batch * over(rows, kSizeRows[s]) * over(cols, kSizeCols[s]) >= (half ? 2 : 1) * kCus) return s;
+    return kSmall;
+}
+template <class F>
+void with_size(Size s, F f) {
+    if (s == kLarge) f(std::integral_constant<Size, kLarge>());
+    else if (s == kMiddle) f(std::integral_constant<Size, kMiddle>());
+    else f(std::integral_constant<Size, kSmall>());
+}
+
+// The power of two that brings `most` to 2^13 .. 2^14 (of what is far below one, less near).
+int scale_for(double most) { return most > 0.0 ? std::min(13 - std::ilogb(most), 24) : 24; }
 
 }  // namespace
 
@@ -115,38 +251,91 @@ double polynomial_bound(double a, double b, double c, double s) {
 const char* orthogonal_fault(int batch, int K, int C) {
     if (K > 32768 || C > 32768) return "matrices of more than 32768 rows or columns";
     if (batch > 65535) return "more than 65535 matrices";
+    if (over(K, 64) * over(C, 64) * batch > 0x7fffffff || over(std::min(K, C), 64) * over(std::min(K, C), 64) * batch > 0x7fffffff)
+        return "more result tiles than one launch holds";
     return "";
 }
 
-size_t orthogonal_scratch(int batch, int K, int C) {
-    const size_t r = std::min(K, C), s = std::max(K, C);
-    return (size_t)batch * (2 * r * s + 2 * r * r) * sizeof(float);
+namespace {
+struct Layout { int64_t x, s, bytes; };               // elements of a plane of X and of S, and of everything
+Layout layout(int64_t batch, int64_t K, int64_t C) {
+    const int64_t r = std::min(K, C);
+    Layout l;
+    l.x = batch * K * round8(C);
+    l.s = batch * r * round8(r);
+    l.bytes = 8 * kNormBlocks * batch + 2 * (2 * 2 * l.x + 2 * 2 * l.s) + 5 * 256;
+    return l;
 }
+}  // namespace
+
+size_t orthogonal_scratch(int batch, int K, int C) { return layout(batch, K, C).bytes; }
 
 void launch_orthogonalise(hipStream_t s, int type, const Orthogonal& a) {
-    const int r = std::min(a.K, a.C), w = std::max(a.K, a.C);
-    float* X = (float*)a.scratch;
-    float* Y = X + (size_t)a.batch * r * w;
-    float* S = Y + (size_t)a.batch * r * w;
-    float* P = S + (size_t)a.batch * r * r;
+    const int r = std::min(a.K, a.C), w = std::max(a.K, a.C), ld = (int)round8(a.C), lds = (int)round8(r);
+    const bool wide = a.K <= a.C;
+    const Layout l = layout(a.batch, a.K, a.C);
+    char* at = (char*)a.scratch;
+    auto take = [&](int64_t bytes) { char* p = at; at += over(bytes, 256) * 256; return p; };
+    double* norms = (double*)take(8 * kNormBlocks * (int64_t)a.batch);
+    Stack X{(_Float16*)take(4 * l.x), l.x, (int64_t)a.K * ld, ld}, Y{(_Float16*)take(4 * l.x), l.x, (int64_t)a.K * ld, ld};
+    Stack S{(_Float16*)take(4 * l.s), l.s, (int64_t)r * lds, lds}, Q{(_Float16*)take(4 * l.s), l.s, (int64_t)r * lds, lds};
+
+    double bound = 1.0;
+    int ex = scale_for(bound);
+    const int64_t count = (int64_t)a.K * a.C;
     auto begin = [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        orthogonal_begin_kernel<T><<<dim3(a.batch), dim3(256), 0, s>>>((const T*)a.G, a.M, a.mu, a.nesterov, a.K, a.C, a.eps, X);
+        const Source<T> src{(const T*)a.G, a.M, a.mu, a.nesterov};
+        const int nb = (int)std::min<int64_t>(over(count, 1024), kNormBlocks);
+        orthogonal_norm_kernel<T><<<dim3(nb, a.batch), dim3(256), 0, s>>>(src, count, norms);
+        orthogonal_begin_kernel<T><<<dim3((unsigned)std::min<int64_t>(over(a.K * (int64_t)(ld / 4), 256), 1024), a.batch), dim3(256), 0, s>>>(
+            src, norms, nb, a.K, a.C, ld, a.eps, std::ldexp(1.f, ex), X.p, X.plane);
     };
     if (type == kBf16) begin((__bf16*)nullptr);
     else if (type == kF16) begin((_Float16*)nullptr);
     else begin((float*)nullptr);
-    const unsigned tr = (r + ST - 1) / ST, tw = (w + ST - 1) / ST;
+
+    const Size square = size_of(a.batch, r, r, true), apply = size_of(a.batch, a.K, a.C, false);
     for (int k = 0; k < a.steps; ++k) {
-        orthogonal_product_kernel<true><<<dim3(tr, tr, a.batch), dim3(256), 0, s>>>(X, X, nullptr, S, r, w, r, 0.f, 1.f);
-        orthogonal_product_kernel<true><<<dim3(tr, tr, a.batch), dim3(256), 0, s>>>(S, S, S, P, r, r, r, a.b, a.c);
-        orthogonal_product_kernel<false><<<dim3(tw, tr, a.batch), dim3(256), 0, s>>>(P, X, X, Y, r, r, w, a.a, 1.f);
+        const double s2 = bound * bound, vertex = a.c != 0.f ? -(double)a.b / (2.0 * a.c) : -1.0;
+        auto p = [&](double x) { return std::fabs(a.a + x * (a.b + (double)a.c * x)); };
+        double most = std::max(p(0.0), p(s2));
+        if (vertex > 0.0 && vertex < s2) most = std::max(most, p(vertex));
+        const int es = scale_for(s2), ep = scale_for(most);
+        bound = polynomial_bound(a.a, a.b, a.c, bound);
+        const int en = scale_for(bound);
+        const bool last = k + 1 == a.steps;
+        with_size(square, [&](auto size) {
+            const int tr = (int)over(r, kSizeRows[size]), tc = (int)over(r, kSizeCols[size]);
+            const dim3 grid((unsigned)((int64_t)tr * tc * a.batch));
+            using Along = Sized<decltype(size)::value, kAlong, kAlong>;
+            using Across = Sized<decltype(size)::value, kAcross, kAcross>;
+            const float one = std::ldexp(1.f, es - 2 * ex);
+            if (wide) orthogonal_square_kernel<Along, kAlong><<<grid, dim3(Along::THREADS), 0, s>>>(X, r, w, S, one, 0.f, 0.f, 0, tr, tc);
+            else orthogonal_square_kernel<Across, kAcross><<<grid, dim3(Across::THREADS), 0, s>>>(X, r, w, S, one, 0.f, 0.f, 0, tr, tc);
+            orthogonal_square_kernel<Along, kAlong><<<grid, dim3(Along::THREADS), 0, s>>>(
+                S, r, r, Q, (float)std::ldexp((double)a.c, ep - 2 * es), (float)std::ldexp((double)a.b, ep - es), (float)std::ldexp((double)a.a, ep), 1, tr, tc);
+        });
+        with_size(apply, [&](auto size) {
+            const int tr = (int)over(a.K, kSizeRows[size]), tc = (int)over(a.C, kSizeCols[size]);
+            const dim3 grid((unsigned)((int64_t)tr * tc * a.batch));
+            const float alpha = std::ldexp(1.f, (last ? 0 : en) - ep - ex);
+            const Stack next = last ? Stack{nullptr, 0, 0, 0} : Y;
+            auto go = [&](auto* o) {
+                using O = std::remove_pointer_t<decltype(o)>;
+                const Target<O> target{(O*)a.out, a.W, a.keep, a.rate};
+                using Wide = Sized<decltype(size)::value, kAlong, kAcross>;
+                using Tall = Sized<decltype(size)::value, kAlong, kAlong>;
+                if (wide) orthogonal_apply_kernel<Wide, kAcross, O><<<grid, dim3(Wide::THREADS), 0, s>>>(Q, X, a.K, a.C, r, next, target, alpha, tr, tc);
+                else orthogonal_apply_kernel<Tall, kAlong, O><<<grid, dim3(Tall::THREADS), 0, s>>>(X, Q, a.K, a.C, r, next, target, alpha, tr, tc);
+            };
+            if (!last || a.W || type == kF32) go((float*)nullptr);
+            else if (type == kBf16) go((__bf16*)nullptr);
+            else go((_Float16*)nullptr);
+        });
         std::swap(X, Y);
+        ex = en;
     }
-    const dim3 grid((unsigned)std::min<int64_t>(((int64_t)a.K * a.C + 255) / 256, 1024), a.batch);
-    if (type == kBf16) orthogonal_end_kernel<__bf16><<<grid, dim3(256), 0, s>>>(X, a.K, a.C, (__bf16*)a.out, a.W, a.keep, a.rate);
-    else if (type == kF16) orthogonal_end_kernel<_Float16><<<grid, dim3(256), 0, s>>>(X, a.K, a.C, (_Float16*)a.out, a.W, a.keep, a.rate);
-    else orthogonal_end_kernel<float><<<grid, dim3(256), 0, s>>>(X, a.K, a.C, (float*)a.out, a.W, a.keep, a.rate);
 }
 
 }  // namespace cadmm

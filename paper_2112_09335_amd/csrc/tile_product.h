@@ -44,9 +44,9 @@ template <> struct View<Pair> {
     const _Float16* p; int64_t ld; int rows; int64_t depth; int64_t plane;
 };
 
-template <class T> constexpr int kParts = 1;
-template <> constexpr int kParts<Pair> = 2;
-template <> constexpr int kParts<float> = 3;
+template <class T> inline constexpr int kParts = 1;
+template <> inline constexpr int kParts<Pair> = 2;
+template <> inline constexpr int kParts<float> = 3;
 
 // a chunk of eight elements as loaded
 template <class T> struct Chunk { uintx4 v[1]; };
@@ -327,34 +327,49 @@ struct Product {
     }
 
     // f(row, column, four results) for every quad of the tile, 16 (TN >= 2) or 8 neighbouring lanes along a row.  Every wavefront passes
-    // its results through LDS of its own.
-    template <class F>
-    __device__ __forceinline__ static void drain(floatx16 (&acc)[TM][TN], unsigned short* S, F f) {
+    // its results through LDS of its own.  MIRROR: what f returns goes on to m(column, row, four results of neighbouring rows).
+    template <bool MIRROR, class F, class M>
+    __device__ __forceinline__ static void drain(floatx16 (&acc)[TM][TN], unsigned short* S, F f, M m) {
         constexpr int J = kSlabCols / 32, Q = kSlabCols / 4;
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
         float* C = reinterpret_cast<float*>(S) + wave * 32 * kSlabLd;
+        auto settled = [] {                                             // a wavefront's LDS accesses are done in their order
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        };
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int j0 = 0; j0 < TN; j0 += J) {
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
+                const int r0 = (wm * TM + i) * 32, c0 = (wn * TN + j0) * 32;
+                settled();
 #pragma unroll
                 for (int j = 0; j < J; ++j)
 #pragma unroll
                     for (int r = 0; r < 16; r += 4)
                         *reinterpret_cast<float4*>(C + (lane & 31) * kSlabLd + 32 * j + 2 * r + 4 * (lane >> 5)) =
                             make_float4(acc[i][j0 + j][r], acc[i][j0 + j][r + 1], acc[i][j0 + j][r + 2], acc[i][j0 + j][r + 3]);
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
+                settled();
 #pragma unroll
                 for (int u = 0; u < 32 * Q / 64; ++u) {
                     const int row = (lane + 64 * u) / Q, col = (lane + 64 * u) % Q * 4;
-                    const float4 v = *reinterpret_cast<const float4*>(C + row * kSlabLd + col);
-                    f((wm * TM + i) * 32 + row, (wn * TN + j0) * 32 + col, v);
+                    float4* at = reinterpret_cast<float4*>(C + row * kSlabLd + col);
+                    if constexpr (MIRROR) *at = f(r0 + row, c0 + col, *at);
+                    else f(r0 + row, c0 + col, *at);
+                }
+                if constexpr (MIRROR) {
+                    settled();
+#pragma unroll
+                    for (int u = 0; u < 32 * Q / 64; ++u) {
+                        const int row = lane % 8 * 4, col = lane / 8 + 8 * u;
+                        const float* at = C + row * kSlabLd + col;
+                        m(c0 + col, r0 + row, make_float4(at[0], at[kSlabLd], at[2 * kSlabLd], at[3 * kSlabLd]));
+                    }
                 }
             }
     }
+    template <class F>
+    __device__ __forceinline__ static void drain(floatx16 (&acc)[TM][TN], unsigned short* S, F f) { drain<false>(acc, S, f, [](int, int, float4) {}); }
 };
 
 // One quad of a row of `width` results at column c (c < width), the row at `to`; whole: width and the row's place are multiples of four
