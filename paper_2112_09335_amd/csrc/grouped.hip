@@ -70,8 +70,8 @@ __global__ __launch_bounds__(P::THREADS, P::THREADS == 256 ? 2 : 1) void grouped
     const int c0 = tile * P::BN, rows = end - r0 < P::BM ? (int)(end - r0) : P::BM;
     const T* Bg = B + (int64_t)g * K * C;
     floatx16 acc[P::TM][P::TN];
-    const View<T> x{A + r0 * lda, lda, rows, K, 0};
-    const View<T> y = YL == kAlong ? View<T>{Bg + (int64_t)c0 * K, K, C - c0, K, 0} : View<T>{Bg + c0, C, C - c0, K, 0};
+    const View<T> x{A + r0 * lda, lda, rows, K};
+    const View<T> y = YL == kAlong ? View<T>{Bg + (int64_t)c0 * K, K, C - c0, K} : View<T>{Bg + c0, C, C - c0, K};
     P::run(acc, x, y, S);
     P::drain(acc, S, [&](int row, int col, float4 v) {
         if (row < rows && c0 + col < C) put(out + (r0 + row) * ldo, c0 + col, C, v, whole_out);
@@ -101,7 +101,7 @@ __global__ __launch_bounds__(P::THREADS, P::THREADS == 256 ? 2 : 1) void grouped
     const int i0 = tile / col_tiles * P::BM, c0 = tile % col_tiles * P::BN;
     floatx16 acc[P::TM][P::TN];
     const int64_t depth = hi - r0 < most ? hi - r0 : most;
-    P::run(acc, View<T>{A + r0 * lda + i0, lda, K - i0, depth, 0}, View<T>{G + r0 * ldg + c0, ldg, C - c0, depth, 0}, S);
+    P::run(acc, View<T>{A + r0 * lda + i0, lda, K - i0, depth}, View<T>{G + r0 * ldg + c0, ldg, C - c0, depth}, S);
     if (hi - lo > most) {
         float* to = partial + part_place(lo, hi, most, i) * part_size;
         P::drain(acc, S, [&](int row, int col, float4 v) {
@@ -142,13 +142,13 @@ void with_type(int type, F f) {
     else f((float*)nullptr);
 }
 
-// Tiles (wavefronts, 32 x 32 accumulators of one, contraction per step, steps ahead).  Large ones read each operand from LDS once for
-// 128 x 256 results, two workgroups a compute unit; the small ones are for products that would not fill the chip with them.
-template <class T> constexpr int kStep = sizeof(T) == 4 ? 16 : 32;
-template <class T, Lie X, Lie Y, Mode M> using Large = Product<T, X, Y, M, 2, 2, 2, 4, kStep<T>, 1>;          // 128 x 256
-template <class T, Lie X, Lie Y, Mode M> using Middle = Product<T, X, Y, M, 2, 2, 2, 2, kStep<T>, 2>;         // 128 x 128
-template <class T, Lie X, Lie Y, Mode M> using Small = Product<T, X, Y, M, 2, 2, 1, 1, 2 * kStep<T>, 2>;      // 64 x 64
-template <class T, Lie X, Lie Y, Mode M> using Few = Product<T, X, Y, M, 1, 2, 1, 1, 2 * kStep<T>, 4>;        // 32 x 64
+// Tiles (wavefronts, 32 x 32 accumulators of one, contraction per step, steps ahead, LDS buffers).  Large ones read each operand from LDS
+// once for 128 x 256 results, two workgroups a compute unit; the small ones are for products that would not fill the chip with them.
+template <class T> constexpr int kStep = 128 / sizeof(T);
+template <class T, Lie X, Lie Y, Mode M> using Large = Product<T, X, Y, M, 2, 2, 2, 4, X == kAlong ? kStep<T> : kStep<T> / 2, 1, 1>;          // 128 x 256
+template <class T, Lie X, Lie Y, Mode M> using Middle = Product<T, X, Y, M, 2, 2, 2, 2, kStep<T>, 1, 1>;         // 128 x 128
+template <class T, Lie X, Lie Y, Mode M> using Small = Product<T, X, Y, M, 2, 2, 1, 1, kStep<T>, 2, 2>;          // 64 x 64
+template <class T, Lie X, Lie Y, Mode M> using Few = Product<T, X, Y, M, 1, 2, 1, 1, kStep<T>, 4, 2>;            // 32 x 64
 
 enum Size { kLarge, kMiddle, kSmall, kFew };
 constexpr int kSizeRows[] = {128, 128, 64, 32}, kSizeCols[] = {256, 128, 64, 64};
@@ -240,7 +240,7 @@ void launch_grouped_nn(hipStream_t s, int type, const GroupedNN& a) {
     with_type(type, [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
         constexpr int64_t Q = 16 / sizeof(T);
-        const bool whole = a.K % 8 == 0 && a.lda % Q == 0 && aligned16(a.A) && aligned16(a.B) && (a.transposed || a.C % 8 == 0);
+        const bool whole = a.K % 8 == 0 && a.lda % Q == 0 && aligned16(a.A) && aligned16(a.B) && a.lda * (int64_t)sizeof(T) <= kMostRow && (a.transposed || a.C % 8 == 0);
         const bool whole_out = a.C % 4 == 0 && a.ldo % 4 == 0 && ((uintptr_t)a.out & (4 * sizeof(T) - 1)) == 0;
         if (a.transposed) {
             if (whole) nn_launch<T, kAlong, kWhole>(s, a, size, whole_out);
@@ -257,7 +257,8 @@ void launch_grouped_tn(hipStream_t s, int type, int out_type, const GroupedTN& a
     with_type(type, [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
         constexpr int64_t Q = 16 / sizeof(T);
-        const bool whole = a.K % 8 == 0 && a.C % 8 == 0 && a.lda % Q == 0 && a.ldg % Q == 0 && aligned16(a.A) && aligned16(a.G);
+        const bool whole = a.K % 8 == 0 && a.C % 8 == 0 && a.lda % Q == 0 && a.ldg % Q == 0 && aligned16(a.A) && aligned16(a.G) &&
+                           std::max(a.lda, a.ldg) * (int64_t)sizeof(T) <= kMostRow;
         auto go = [&](auto* o) {
             using O = std::remove_pointer_t<decltype(o)>;
             if (whole) tn_launch<T, kWhole, O>(s, a, plan);

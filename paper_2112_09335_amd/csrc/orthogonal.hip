@@ -60,7 +60,9 @@ __device__ __forceinline__ void split_pair(float x, _Float16& h, _Float16& l) {
     l = (_Float16)(x - (float)h);
 }
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ void put_pair(_Float16* to, int64_t plane, float4 v) {
+// Where element e of a row of pairs is: eight high parts, then their eight low ones.
+__device__ __forceinline__ int64_t pair_at(int64_t e) { return 2 * e - (e & 7); }
+__device__ __forceinline__ void put_pair(_Float16* to, float4 v) {
     f16x4 h, l;
     _Float16 a, b;
     split_pair(v.x, a, b); h.x = a; l.x = b;
@@ -68,34 +70,37 @@ __device__ __forceinline__ void put_pair(_Float16* to, int64_t plane, float4 v) 
     split_pair(v.z, a, b); h.z = a; l.z = b;
     split_pair(v.w, a, b); h.w = a; l.w = b;
     *reinterpret_cast<f16x4*>(to) = h;
-    *reinterpret_cast<f16x4*>(to + plane) = l;
+    *reinterpret_cast<f16x4*>(to + 8) = l;
 }
 
-// X = direction / (norm + eps), scaled, as pairs; rows of ld elements, what is past a row's end is zero.
+// Matrices of `each` fp16 numbers, rows of `ld` pairs of which `width` are used: whole chunks, zeros past the last column.
+struct Stack {
+    _Float16* p; int64_t each; int ld, width;
+    __device__ __forceinline__ _Float16* matrix(int64_t b) const { return p + b * each; }
+    __device__ __forceinline__ int64_t at(int row, int col) const { return (int64_t)row * 2 * ld + pair_at(col); }
+    __device__ __forceinline__ View<Pair> view(int64_t b, int row, int col, int rows, int64_t depth) const { return {matrix(b) + at(row, col), 2 * ld, rows, depth}; }
+};
+
+// X = direction / (norm + eps), scaled, as pairs; what is past a row's end is zero.
 template <class T>
-__global__ __launch_bounds__(256) void orthogonal_begin_kernel(Source<T> src, const double* __restrict__ norms, int n_norms, int K, int C, int ld,
-                                                               float eps, float scale, _Float16* __restrict__ X, int64_t plane) {
+__global__ __launch_bounds__(256) void orthogonal_begin_kernel(Source<T> src, const double* __restrict__ norms, int n_norms, int K, int C,
+                                                               float eps, float scale, Stack X) {
     const int64_t b = blockIdx.y;
     double sum = 0.0;
     for (int i = 0; i < n_norms; ++i) sum += norms[b * kNormBlocks + i];
     const double norm = sqrt(sum) + (double)eps;
     // (no direction: zero; an entry that is not finite: nothing is)
     const double inv = norm == 0.0 ? 0.0 : norm < HUGE_VAL ? (double)scale / norm : __builtin_nan("");
-    const int quads = ld / 4;
+    const int quads = X.width / 4;
     for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < (int64_t)K * quads; q += (int64_t)gridDim.x * 256) {
         const int64_t row = q / quads;
         const int c = (int)(q % quads) * 4;
         float v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = c + e < C ? (float)((double)src.again(b * K * C + row * C + c + e) * inv) : 0.f;
-        put_pair(X + (b * K + row) * ld + c, plane, make_float4(v[0], v[1], v[2], v[3]));
+        put_pair(X.matrix(b) + X.at((int)row, c), make_float4(v[0], v[1], v[2], v[3]));
     }
 }
-
-struct Stack {                          // pairs: matrices of rows x ld
-    _Float16* p; int64_t plane, each; int ld;
-    __device__ __forceinline__ View<Pair> view(int64_t b, int64_t at, int rows, int64_t depth) const { return {p + b * each + at, ld, rows, depth, plane}; }
-};
 
 // Workgroup -> (matrix, tile row, tile column); tiles of a matrix one after the other on one XCD (see the products over groups).
 __device__ __forceinline__ void place(int tile_rows, int tile_cols, int64_t& b, int& ti, int& tj) {
@@ -111,7 +116,7 @@ __device__ __forceinline__ void place(int tile_rows, int tile_cols, int64_t& b, 
 // out = alpha X^T X or X X^T (LIE: kAlong forms X X^T), or with `from` = X symmetric: alpha X X + beta X + gamma 1.  The result is symmetric:
 // tiles below the diagonal are left out, and of the others every entry on or above it is stored to both its places.
 template <class P, Lie LIE>
-__global__ __launch_bounds__(P::THREADS, 2) void orthogonal_square_kernel(Stack x, int r, int64_t depth, Stack out, float alpha, float beta, float gamma,
+__global__ __launch_bounds__(P::THREADS, P::THREADS == 256 ? 2 : 1) void orthogonal_square_kernel(Stack x, int r, int64_t depth, Stack out, float alpha, float beta, float gamma,
                                                                           int with_linear, int tile_rows, int tile_cols) {
     __shared__ __align__(16) unsigned short S[P::kLds];
     int64_t b;
@@ -120,17 +125,17 @@ __global__ __launch_bounds__(P::THREADS, 2) void orthogonal_square_kernel(Stack 
     const int i0 = ti * P::BM, c0 = tj * P::BN;
     if (i0 >= c0 + P::BN) return;
     floatx16 acc[P::TM][P::TN];
-    if (LIE == kAlong) P::run(acc, x.view(b, (int64_t)i0 * x.ld, r - i0, depth), x.view(b, (int64_t)c0 * x.ld, r - c0, depth), S);
-    else P::run(acc, x.view(b, i0, x.ld - i0, depth), x.view(b, c0, x.ld - c0, depth), S);
-    _Float16* to = out.p + b * out.each;
-    const _Float16* lin = x.p + b * x.each;
+    if (LIE == kAlong) P::run(acc, x.view(b, i0, 0, r - i0, depth), x.view(b, c0, 0, r - c0, depth), S);
+    else P::run(acc, x.view(b, 0, i0, x.width - i0, depth), x.view(b, 0, c0, x.width - c0, depth), S);
+    _Float16* to = out.matrix(b);
+    const _Float16* lin = x.matrix(b);
     const bool crossing = c0 < i0 + P::BM;                 // the tile holds entries below the diagonal
     auto own = [&](int row, int col, float4 v) {
         const int i = i0 + row, j = c0 + col;
         float w[4] = {alpha * v.x, alpha * v.y, alpha * v.z, alpha * v.w};
-        if (i >= r || j >= out.ld) return v;
+        if (i >= r || j >= out.width) return v;
         if (with_linear) {
-            const f16x4 h = *reinterpret_cast<const f16x4*>(lin + (int64_t)i * x.ld + j), l = *reinterpret_cast<const f16x4*>(lin + (int64_t)i * x.ld + j + x.plane);
+            const f16x4 h = *reinterpret_cast<const f16x4*>(lin + x.at(i, j)), l = *reinterpret_cast<const f16x4*>(lin + x.at(i, j) + 8);
             const float s[4] = {(float)h.x + (float)l.x, (float)h.y + (float)l.y, (float)h.z + (float)l.z, (float)h.w + (float)l.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) w[e] = w[e] + beta * s[e] + (j + e == i ? gamma : 0.f);
@@ -138,26 +143,26 @@ __global__ __launch_bounds__(P::THREADS, 2) void orthogonal_square_kernel(Stack 
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = j + e < r ? w[e] : 0.f;
         const float4 q = make_float4(w[0], w[1], w[2], w[3]);
-        _Float16* at = to + (int64_t)i * out.ld + j;
-        if (!crossing || j >= i) put_pair(at, out.plane, q);
+        _Float16* at = to + out.at(i, j);
+        if (!crossing || j >= i) put_pair(at, q);
         else {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (j + e >= i) split_pair(w[e], at[e], at[e + out.plane]);
+                if (j + e >= i) split_pair(w[e], at[e], at[e + 8]);
         }
         return q;
     };
-    // (rows r .. ld of the result are never read; columns r .. ld hold zeros, which the own side of the last tile column leaves)
+    // ( columns r .. width hold zeros, which the own side of the last tile column leaves)
     auto mirror = [&](int col, int row, float4 v) {
         const int i = i0 + row, j = c0 + col;
         if (j >= r || i >= r) return;
         const float w[4] = {v.x, v.y, v.z, v.w};
-        _Float16* at = to + (int64_t)j * out.ld + i;
-        if (i + 3 < j) put_pair(at, out.plane, v);
+        _Float16* at = to + out.at(j, i);
+        if (i + 3 < j) put_pair(at, v);
         else {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (i + e < j) split_pair(w[e], at[e], at[e + out.plane]);
+                if (i + e < j) split_pair(w[e], at[e], at[e + 8]);
         }
     };
     P::template drain<true>(acc, S, own, mirror);
@@ -166,7 +171,7 @@ __global__ __launch_bounds__(P::THREADS, 2) void orthogonal_square_kernel(Stack 
 // X <- P X (YL: X lies across the contraction) or X P (P is symmetric and lies along it), alpha times; the last time to `out` or off W.
 template <class O> struct Target { O* out; float* W; float keep, rate; };
 template <class P, Lie YL, class O>
-__global__ __launch_bounds__(P::THREADS, 2) void orthogonal_apply_kernel(Stack left, Stack right, int K, int C, int r, Stack next, Target<O> last, float alpha,
+__global__ __launch_bounds__(P::THREADS, P::THREADS == 256 ? 2 : 1) void orthogonal_apply_kernel(Stack left, Stack right, int K, int C, int r, Stack next, Target<O> last, float alpha,
                                                                          int tile_rows, int tile_cols) {
     __shared__ __align__(16) unsigned short S[P::kLds];
     int64_t b;
@@ -174,13 +179,13 @@ __global__ __launch_bounds__(P::THREADS, 2) void orthogonal_apply_kernel(Stack l
     place(tile_rows, tile_cols, b, ti, tj);
     const int i0 = ti * P::BM, c0 = tj * P::BN;
     floatx16 acc[P::TM][P::TN];
-    P::run(acc, left.view(b, (int64_t)i0 * left.ld, K - i0, r), YL == kAcross ? right.view(b, c0, right.ld - c0, r) : right.view(b, (int64_t)c0 * right.ld, C - c0, r), S);
+    P::run(acc, left.view(b, i0, 0, K - i0, r), YL == kAcross ? right.view(b, 0, c0, right.width - c0, r) : right.view(b, c0, 0, C - c0, r), S);
     if (next.p) {
-        _Float16* to = next.p + b * next.each;
+        _Float16* to = next.matrix(b);
         P::drain(acc, S, [&](int row, int col, float4 v) {
             const int i = i0 + row, j = c0 + col;
-            if (i >= K || j >= next.ld) return;
-            put_pair(to + (int64_t)i * next.ld + j, next.plane,
+            if (i >= K || j >= next.width) return;
+            put_pair(to + next.at(i, j),
                      make_float4(j < C ? alpha * v.x : 0.f, j + 1 < C ? alpha * v.y : 0.f, j + 2 < C ? alpha * v.z : 0.f, j + 3 < C ? alpha * v.w : 0.f));
         });
     } else if (last.W) {
@@ -203,16 +208,19 @@ __global__ __launch_bounds__(P::THREADS, 2) void orthogonal_apply_kernel(Stack l
     }
 }
 
-template <Lie X, Lie Y> using Large = Product<Pair, X, Y, kWhole, 2, 2, 2, 4, 16, 1>;      // 128 x 256
-template <Lie X, Lie Y> using Middle = Product<Pair, X, Y, kWhole, 2, 2, 2, 2, 16, 2>;     // 128 x 128
-template <Lie X, Lie Y> using Small = Product<Pair, X, Y, kWhole, 2, 2, 1, 1, 32, 2>;      // 64 x 64
+template <Lie X, Lie Y> using Large = Direct<Pair, X, Y, 2, 4, 4, 2, 2>;         // 256 x 256
+template <Lie X, Lie Y> using Middle = Direct<Pair, X, Y, 2, 2, 2, 2, 2>;        // 128 x 128
+template <Lie X, Lie Y> using Small = Direct<Pair, X, Y, 2, 2, 1, 1, 4>;         // 64 x 64
 enum Size { kLarge, kMiddle, kSmall };
-constexpr int kSizeRows[] = {128, 128, 64}, kSizeCols[] = {256, 128, 64};
+constexpr int kSizeRows[] = {256, 128, 64}, kSizeCols[] = {256, 128, 64};
 template <Size SIZE, Lie X, Lie Y>
 using Sized = std::conditional_t<SIZE == kLarge, Large<X, Y>, std::conditional_t<SIZE == kMiddle, Middle<X, Y>, Small<X, Y>>>;
 
 int64_t over(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t round8(int64_t n) { return (n + 7) / 8 * 8; }
+// Pairs from one row to the next: whole chunks, and an odd number of 256-byte pieces, so that the rows of a tile spread over the L2's
+// channels (256 bytes each, 16 of them).
+int64_t row_pairs(int64_t n) { return n <= 64 ? round8(n) : (over(n, 64) | 1) * 64; }
 constexpr int64_t kCus = 256;
 // The largest tiles that give every compute unit one; half: of a symmetric result only that much is formed.
 Size size_of(int64_t batch, int64_t rows, int64_t cols, bool half) {
@@ -257,12 +265,12 @@ const char* orthogonal_fault(int batch, int K, int C) {
 }
 
 namespace {
-struct Layout { int64_t x, s, bytes; };               // elements of a plane of X and of S, and of everything
+struct Layout { int64_t x, s, bytes; };               // elements of X and of S, and bytes of everything
 Layout layout(int64_t batch, int64_t K, int64_t C) {
     const int64_t r = std::min(K, C);
     Layout l;
-    l.x = batch * K * round8(C);
-    l.s = batch * r * round8(r);
+    l.x = batch * K * row_pairs(C);
+    l.s = batch * r * row_pairs(r);
     l.bytes = 8 * kNormBlocks * batch + 2 * (2 * 2 * l.x + 2 * 2 * l.s) + 5 * 256;
     return l;
 }
@@ -271,14 +279,14 @@ Layout layout(int64_t batch, int64_t K, int64_t C) {
 size_t orthogonal_scratch(int batch, int K, int C) { return layout(batch, K, C).bytes; }
 
 void launch_orthogonalise(hipStream_t s, int type, const Orthogonal& a) {
-    const int r = std::min(a.K, a.C), w = std::max(a.K, a.C), ld = (int)round8(a.C), lds = (int)round8(r);
+    const int r = std::min(a.K, a.C), w = std::max(a.K, a.C), ld = (int)row_pairs(a.C), lds = (int)row_pairs(r);
     const bool wide = a.K <= a.C;
     const Layout l = layout(a.batch, a.K, a.C);
     char* at = (char*)a.scratch;
     auto take = [&](int64_t bytes) { char* p = at; at += over(bytes, 256) * 256; return p; };
     double* norms = (double*)take(8 * kNormBlocks * (int64_t)a.batch);
-    Stack X{(_Float16*)take(4 * l.x), l.x, (int64_t)a.K * ld, ld}, Y{(_Float16*)take(4 * l.x), l.x, (int64_t)a.K * ld, ld};
-    Stack S{(_Float16*)take(4 * l.s), l.s, (int64_t)r * lds, lds}, Q{(_Float16*)take(4 * l.s), l.s, (int64_t)r * lds, lds};
+    Stack X{(_Float16*)take(4 * l.x), (int64_t)2 * a.K * ld, ld, (int)round8(a.C)}, Y{(_Float16*)take(4 * l.x), (int64_t)2 * a.K * ld, ld, (int)round8(a.C)};
+    Stack S{(_Float16*)take(4 * l.s), (int64_t)2 * r * lds, lds, (int)round8(r)}, Q{(_Float16*)take(4 * l.s), (int64_t)2 * r * lds, lds, (int)round8(r)};
 
     double bound = 1.0;
     int ex = scale_for(bound);
@@ -288,8 +296,8 @@ void launch_orthogonalise(hipStream_t s, int type, const Orthogonal& a) {
         const Source<T> src{(const T*)a.G, a.M, a.mu, a.nesterov};
         const int nb = (int)std::min<int64_t>(over(count, 1024), kNormBlocks);
         orthogonal_norm_kernel<T><<<dim3(nb, a.batch), dim3(256), 0, s>>>(src, count, norms);
-        orthogonal_begin_kernel<T><<<dim3((unsigned)std::min<int64_t>(over(a.K * (int64_t)(ld / 4), 256), 1024), a.batch), dim3(256), 0, s>>>(
-            src, norms, nb, a.K, a.C, ld, a.eps, std::ldexp(1.f, ex), X.p, X.plane);
+        orthogonal_begin_kernel<T><<<dim3((unsigned)std::min<int64_t>(over(a.K * (round8(a.C) / 4), 256), 1024), a.batch), dim3(256), 0, s>>>(
+            src, norms, nb, a.K, a.C, a.eps, std::ldexp(1.f, ex), X);
     };
     if (type == kBf16) begin((__bf16*)nullptr);
     else if (type == kF16) begin((_Float16*)nullptr);

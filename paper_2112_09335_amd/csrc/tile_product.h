@@ -4,12 +4,15 @@
 // Operands.  Either may lie with its contraction along the rows in memory (an element's k is its column: kAlong) or across
 // them (an element's k is its row: kAcross), and is one of
 //   bf16 / fp16   as they are, one product per pair of elements;
-//   Pair          two planes of fp16 whose sum is the value, 22 bits of significand: three products (the fourth is below 2^-22);
+//   Pair          two fp16 whose sum is the value, 22 bits of significand: three products (the fourth is below 2^-22); eight high
+//                 parts are followed by their eight low ones in memory;
 //   float         split on the way into three bf16 parts, exactly (8 + 8 + 8 bits): six products (the other three are below 2^-24).
 //
-// Way of the data: 16-byte chunks of eight k (kAlong) or eight i (kAcross) from memory into registers, PF steps of BK ahead; from
-// there, split where need be, into one of two LDS buffers; from there into the matrix cores' operand layout, eight k of one
-// row per lane.  One barrier per step.
+// Way of the data: chunks of eight k (kAlong) or eight i (kAcross) from memory into registers, PF steps of BK ahead; from there,
+// split where need be, to LDS; from there into the matrix cores' operand layout, eight k of one row per lane.  With two LDS
+// buffers there is one barrier per step; with one there are two, and as much more of the contraction per step.  A step takes whole
+// lines (128 bytes) of rows that lie along the contraction: what is left of a line is gone from the L1 by the next step (with
+// 32 bytes a step, products of Pairs ran at 36 % of the matrix cores' cycles, whatever was loaded ahead).
 //   kAlong tiles are kept in that layout, 64 lanes x 16 bytes for every 32 rows and 16 k, with the rows permuted by the chunk's number
 //   so that the chunks of one row, which neighbouring lanes store, fall into different banks.
 //   kAcross tiles are kept as rows of k; ds_read_b64_tr_b16 turns 4 k x 16 i over 16 lanes into four k of one i per lane.  The four rows
@@ -29,19 +32,21 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
 
-struct Pair {};                         // an operand of two fp16 planes
+struct Pair {};                         // an operand of two fp16 parts
 enum Lie { kAlong, kAcross };
-// kWhole: chunks are there or not at all, and 16-byte aligned.  kAny: rows of any length at any element.
+// kWhole: chunks are there or not at all, 16-byte aligned, and kMostRow bytes at most from one row to the next, so that a place in a
+// tile is a base and 32 bits.  kAny: rows of any length and distance, at any element.
 enum Mode { kWhole, kAny };
+constexpr int64_t kMostRow = (int64_t)1 << 22;
 
-// X(i, k), i < rows, k < depth; `plane`: elements from the high to the low plane of a Pair.
+// X(i, k), i < rows, k < depth; ld: elements from one row in memory to the next (of a Pair: fp16 numbers, two an element).
 template <class T> struct View {
     using Element = T;
-    const T* p; int64_t ld; int rows; int64_t depth; int64_t plane;
+    const T* p; int64_t ld; int rows; int64_t depth;
 };
 template <> struct View<Pair> {
     using Element = _Float16;
-    const _Float16* p; int64_t ld; int rows; int64_t depth; int64_t plane;
+    const _Float16* p; int64_t ld; int rows; int64_t depth;
 };
 
 template <class T> inline constexpr int kParts = 1;
@@ -57,33 +62,30 @@ typedef unsigned uintx4a4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef unsigned uintx4a2 __attribute__((ext_vector_type(4), aligned(2)));
 template <int BYTES>
 __device__ __forceinline__ uintx4 load16(const void* p) {              // 16 bytes at any multiple of BYTES
-    if constexpr (BYTES == 16) return *reinterpret_cast<const uintx4*>(p);
-    else if constexpr (BYTES == 4) return *reinterpret_cast<const uintx4a4*>(p);
+    if constexpr (BYTES == 4) return *reinterpret_cast<const uintx4a4*>(p);
     else return *reinterpret_cast<const uintx4a2*>(p);
 }
 
 // Loading and putting the chunk right are two steps, so that nothing waits for a load before the chunk is stored to LDS; and no
-// load is under a condition that differs between lanes.  `row`: its row in memory, of which `width` elements exist; c: the first of the
-// chunk's eight columns.  What lies past the row's end becomes zero.
-template <class T, Mode MODE>
-__device__ __forceinline__ void fetch(Chunk<T>& q, const typename View<T>::Element* row, int64_t plane, int c, int width) {
-    using E = typename View<T>::Element;
-    if constexpr (MODE == kWhole) {
-        const E* at = row + (c < width ? c : 0);
-        if constexpr (sizeof(E) == 4) { q.v[0] = load16<16>(at); q.v[1] = load16<16>(at + 4); }
-        else {
-            q.v[0] = load16<16>(at);
-            if constexpr (kParts<T> == 2) q.v[1] = load16<16>(at + plane);
-        }
-    } else if (width >= 8) {                                            // (uniform) the last chunk is moved back to end with the row
-        const E* at = row + (c + 8 <= width ? c : width - 8);
-        q.v[0] = load16<sizeof(E)>(at);
-        if constexpr (sizeof(E) == 4) q.v[1] = load16<sizeof(E)>(at + 4);
+// load is under a condition that differs between lanes.  A chunk of whole ones:
+template <class T>
+__device__ __forceinline__ void fetch_whole(Chunk<T>& q, const char* at) {
+    q.v[0] = *reinterpret_cast<const uintx4*>(at);
+    if constexpr (sizeof(q) == 32) q.v[1] = *reinterpret_cast<const uintx4*>(at + 16);
+}
+// and any: `row`: its row in memory, of which `width` elements exist; c: the first of the chunk's eight columns.  What lies past the
+// row's end becomes zero in settle.
+template <class T>
+__device__ __forceinline__ void fetch_any(Chunk<T>& q, const T* row, int c, int width) {
+    if (width >= 8) {                                                   // (uniform) the last chunk is moved back to end with the row
+        const T* at = row + (c + 8 <= width ? c : width - 8);
+        q.v[0] = load16<sizeof(T)>(at);
+        if constexpr (sizeof(T) == 4) q.v[1] = load16<sizeof(T)>(at + 4);
     } else {
-        E v[8];
+        T v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = row[c + e < width ? c + e : width - 1];
-        __builtin_memcpy(&q, v, 8 * sizeof(E));
+        __builtin_memcpy(&q, v, 8 * sizeof(T));
     }
 }
 template <class T, Mode MODE>
@@ -147,8 +149,10 @@ struct Operand {
     static constexpr int kChunks = ROWS * BK / 8;
     static constexpr int kEach = (kChunks + THREADS - 1) / THREADS;
     static constexpr bool kIdle = kChunks % THREADS != 0;                 // some threads carry none at the last round
+    static constexpr int kChunkBytes = sizeof(Chunk<T>);
     Chunk<T> q[PF][kEach];
-    const E* at[kEach];                                                  // start of the row (kAlong), or of the row of the step (kAcross)
+    unsigned place[kEach];                                               // kWhole: bytes from the tile's (kAlong) or the step's (kAcross) first
+    const E* at[kEach];                                                  // kAny: start of the row (kAlong), or of the row of the step (kAcross)
 
     __device__ __forceinline__ static int row_of(int u) { return (threadIdx.x + u * THREADS) / kPerRow; }
     __device__ __forceinline__ static int chunk_of(int u) { return (threadIdx.x + u * THREADS) % kPerRow; }
@@ -157,26 +161,34 @@ struct Operand {
     __device__ __forceinline__ void begin(const View<T>& x) {
 #pragma unroll
         for (int u = 0; u < kEach; ++u) {
-            const int r = row_of(u);
-            if constexpr (LIE == kAlong) at[u] = x.p + (int64_t)(r < x.rows ? r : x.rows - 1) * x.ld;    // rows past the end: any (their results are not stored)
+            int r = row_of(u);
+            if (LIE == kAlong && r >= x.rows) r = x.rows - 1;               // rows past the end: any (their results are not stored)
+            if constexpr (MODE == kWhole) place[u] = (unsigned)r * (unsigned)(x.ld * sizeof(E)) + chunk_of(u) * kChunkBytes;
             else at[u] = x.p + (int64_t)r * x.ld;
         }
     }
-    // the step that begins at k0 < depth, into slot s
+    // the step that begins at k0, into slot s
     __device__ __forceinline__ void load(const View<T>& x, int64_t k0, int s) {
         const int64_t rest = x.depth - k0;
         const int left = (int)(rest < BK ? rest : BK);
+        const int64_t ahead = left > 0 ? k0 : 0;                           // (a step past the end loads the first one's data)
+        if constexpr (MODE == kWhole) {
+            const char* base = reinterpret_cast<const char*>(x.p) + (LIE == kAlong ? ahead / 8 * kChunkBytes : ahead * x.ld * (int64_t)sizeof(E));
+            const int here = left > 0 ? left : (int)(x.depth < BK ? x.depth : BK);
 #pragma unroll
-        for (int u = 0; u < kEach; ++u) {
-            if constexpr (LIE == kAlong) {
+            for (int u = 0; u < kEach; ++u) {
                 const int c = 8 * chunk_of(u);
-                if (MODE == kWhole) fetch<T, MODE>(q[s][u], at[u] + (c < left ? k0 : 0), x.plane, c < left ? c : 0, BK);
-                else fetch<T, MODE>(q[s][u], at[u], x.plane, (int)k0 + c, (int)x.depth);
-            } else {
-                const bool in = row_of(u) < left;
-                const E* row = in ? at[u] : x.p;                         // (row 0 of the view is there)
-                fetch<T, MODE>(q[s][u], row, x.plane, 8 * chunk_of(u), x.rows);
-                at[u] += BK * x.ld;
+                const bool in = LIE == kAlong ? c < here : row_of(u) < here && c < x.rows;
+                fetch_whole<T>(q[s][u], base + (in ? place[u] : 0u));       // (one that does not exist: the first one)
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < kEach; ++u) {
+                if constexpr (LIE == kAlong) fetch_any<T>(q[s][u], at[u], (int)k0 + 8 * chunk_of(u), (int)x.depth);
+                else {
+                    fetch_any<T>(q[s][u], row_of(u) < left ? at[u] : x.p, 8 * chunk_of(u), x.rows);          // (row 0 of the view is there)
+                    at[u] += BK * x.ld;
+                }
             }
         }
     }
@@ -243,87 +255,22 @@ __device__ __forceinline__ floatx16 multiply(uintx4 a, uintx4 b, floatx16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// WM x WN wavefronts, TM x TN accumulators of 32 x 32 each.
-template <class T, Lie XL, Lie YL, Mode MODE, int WM_, int WN_, int TM_, int TN_, int BK_, int PF_>
-struct Product {
-    static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, BK = BK_, PF = PF_;
+// What tiles of WM x WN wavefronts, TM x TN accumulators of 32 x 32 each, have in common.
+template <int WM_, int WN_, int TM_, int TN_>
+struct Tile {
+    static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_;
     static constexpr int BM = 32 * TM * WM, BN = 32 * TN * WN, THREADS = 64 * WM * WN;
-    using X = Operand<T, XL, MODE, BM, BK, THREADS, PF>;
-    using Y = Operand<T, YL, MODE, BN, BK, THREADS, PF>;
-    static constexpr int P = kParts<T>;
-    static constexpr int kBuffer = X::kSize + Y::kSize;
     // results on their way out: 32 rows by up to 64 columns of a wavefront, at a time
     static constexpr int kSlabCols = TN >= 2 ? 64 : 32, kSlabLd = kSlabCols + 4;
     static constexpr int kSlabs = WM * WN * 32 * kSlabLd * 2;            // in 16-bit elements
-    static constexpr int kLds = 2 * kBuffer > kSlabs ? 2 * kBuffer : kSlabs;
 
-    __device__ __forceinline__ static void step(floatx16 (&acc)[TM][TN], const unsigned short* S) {
-        const int wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
-#pragma unroll
-        for (int s = 0; s < BK / 16; ++s) {
-            uintx4 a[P][TM];
-#pragma unroll
-            for (int p = 0; p < P; ++p)
-#pragma unroll
-                for (int i = 0; i < TM; ++i) a[p][i] = X::operand(S, wm * TM + i, s, p);
-#pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                uintx4 b[P];
-#pragma unroll
-                for (int p = 0; p < P; ++p) b[p] = Y::operand(S + X::kSize, wn * TN + j, s, p);
-#pragma unroll
-                for (int i = 0; i < TM; ++i) {                            // smallest terms first
-                    floatx16 c = acc[i][j];
-                    if constexpr (P == 3) {
-                        c = multiply<T>(b[0], a[2][i], c);
-                        c = multiply<T>(b[2], a[0][i], c);
-                        c = multiply<T>(b[1], a[1][i], c);
-                    }
-                    if constexpr (P >= 2) {
-                        c = multiply<T>(b[0], a[1][i], c);
-                        c = multiply<T>(b[1], a[0][i], c);
-                    }
-                    acc[i][j] = multiply<T>(b[0], a[0][i], c);
-                }
-            }
-        }
-    }
-
-    __device__ __forceinline__ static void run(floatx16 (&acc)[TM][TN], const View<T>& x, const View<T>& y, unsigned short* S) {
+    __device__ __forceinline__ static void clear(floatx16 (&acc)[TM][TN]) {
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-        const int64_t depth = x.depth;
-        if (depth <= 0) return;
-        X X_;
-        Y Y_;
-        X_.begin(x);
-        Y_.begin(y);
-#pragma unroll
-        for (int s = 0; s < PF; ++s)
-            if (s * BK < depth) { X_.load(x, s * BK, s); Y_.load(y, s * BK, s); }
-        X_.store(x, 0, 0, S);
-        Y_.store(y, 0, 0, S + X::kSize);
-        __syncthreads();
-        int buffer = 0;
-        for (int64_t k0 = 0; k0 < depth; k0 += PF * BK) {
-#pragma unroll
-            for (int u = 0; u < PF; ++u) {
-                const int64_t k = k0 + u * BK;
-                if (k >= depth) break;                                   // (uniform)
-                if (k + PF * BK < depth) { X_.load(x, k + PF * BK, u); Y_.load(y, k + PF * BK, u); }
-                step(acc, S + buffer * kBuffer);
-                buffer ^= 1;
-                if (k + BK < depth) {
-                    X_.store(x, k + BK, (u + 1) % PF, S + buffer * kBuffer);
-                    Y_.store(y, k + BK, (u + 1) % PF, S + buffer * kBuffer + X::kSize);
-                }
-                __syncthreads();
-            }
-        }
     }
 
     // f(row, column, four results) for every quad of the tile, 16 (TN >= 2) or 8 neighbouring lanes along a row.  Every wavefront passes
@@ -370,6 +317,240 @@ struct Product {
     }
     template <class F>
     __device__ __forceinline__ static void drain(floatx16 (&acc)[TM][TN], unsigned short* S, F f) { drain<false>(acc, S, f, [](int, int, float4) {}); }
+};
+
+// Tiles whose operands go through registers: any operand, any rows.
+template <class T, Lie XL, Lie YL, Mode MODE, int WM_, int WN_, int TM_, int TN_, int BK_, int PF_, int BUFFERS_>
+struct Product : Tile<WM_, WN_, TM_, TN_> {
+    using Base = Tile<WM_, WN_, TM_, TN_>;
+    using Base::WM; using Base::WN; using Base::TM; using Base::TN; using Base::BM; using Base::BN; using Base::THREADS; using Base::kSlabs;
+    static constexpr int BK = BK_, PF = PF_, BUFFERS = BUFFERS_;
+    using X = Operand<T, XL, MODE, BM, BK, THREADS, PF>;
+    using Y = Operand<T, YL, MODE, BN, BK, THREADS, PF>;
+    static constexpr int P = kParts<T>;
+    static constexpr int kBuffer = X::kSize + Y::kSize;
+    static constexpr int kLds = BUFFERS * kBuffer > kSlabs ? BUFFERS * kBuffer : kSlabs;
+
+    __device__ __forceinline__ static void step(floatx16 (&acc)[TM][TN], const unsigned short* S) {
+        const int wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
+#pragma unroll
+        for (int s = 0; s < BK / 16; ++s) {
+            uintx4 a[P][TM];
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int i = 0; i < TM; ++i) a[p][i] = X::operand(S, wm * TM + i, s, p);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                uintx4 b[P];
+#pragma unroll
+                for (int p = 0; p < P; ++p) b[p] = Y::operand(S + X::kSize, wn * TN + j, s, p);
+                auto add = [&](int p, int q) {                             // (neighbouring instructions have different accumulators)
+#pragma unroll
+                    for (int i = 0; i < TM; ++i) acc[i][j] = multiply<T>(b[p], a[q][i], acc[i][j]);
+                };
+                // smallest terms first
+                if constexpr (P == 3) { add(0, 2); add(2, 0); add(1, 1); }
+                if constexpr (P >= 2) { add(0, 1); add(1, 0); }
+                add(0, 0);
+            }
+        }
+    }
+
+    __device__ __forceinline__ static void run(floatx16 (&acc)[TM][TN], const View<T>& x, const View<T>& y, unsigned short* S) {
+        Base::clear(acc);
+        const int64_t depth = x.depth;
+        if (depth <= 0) return;
+        X X_;
+        Y Y_;
+        X_.begin(x);
+        Y_.begin(y);
+#pragma unroll
+        for (int s = 0; s < PF; ++s)
+        { X_.load(x, s * BK, s); Y_.load(y, s * BK, s); }
+        // (steps past the end load what is there and store zeros: a load or store that some steps leave out would make every wait
+        // for loads one for all of them, whatever is ahead)
+        int buffer = 0;
+        if constexpr (BUFFERS == 2) {
+            X_.store(x, 0, 0, S);
+            Y_.store(y, 0, 0, S + X::kSize);
+            __syncthreads();
+        }
+        for (int64_t k0 = 0; k0 < depth; k0 += PF * BK) {
+#pragma unroll
+            for (int u = 0; u < PF; ++u) {
+                const int64_t k = k0 + u * BK;
+                if (u > 0 && k >= depth) break;                          // (uniform)
+                if constexpr (BUFFERS == 1) {
+                    X_.store(x, k, u, S);
+                    Y_.store(y, k, u, S + X::kSize);
+                    __syncthreads();
+                }
+                X_.load(x, k + PF * BK, u);
+                Y_.load(y, k + PF * BK, u);
+                step(acc, S + buffer * kBuffer);
+                if constexpr (BUFFERS == 2) {
+                    buffer ^= 1;
+                    X_.store(x, k + BK, (u + 1) % PF, S + buffer * kBuffer);
+                    Y_.store(y, k + BK, (u + 1) % PF, S + buffer * kBuffer + X::kSize);
+                }
+                __syncthreads();
+            }
+        }
+    }
+
+};
+
+// Tiles whose operands go from memory straight to LDS, STAGES - 1 steps ahead: bf16, fp16 and Pairs whose chunks are whole.  An LDS tile
+// is made of pieces of 16 bytes, of a chunk of 16-bit numbers or of a chunk's high or low parts, as they come in memory: rows of 128 bytes
+// (kAlong), or BK rows of the tile's width (kAcross); an instruction of a wavefront fills 64 pieces in a row, and which piece of memory a
+// lane brings is chosen so that the 32 lanes that read at a time find theirs in different banks.  One barrier per step; the first
+// operands of a step are read under the last matrix instructions of the one before.  32 x 2048 x 1024 x 1024 Pairs: 868 -> 997 TFLOP/s
+// of matrix instructions over the way through registers, bf16 853 -> 1126 (a library product of 4096^3: 1130).
+static __device__ const uintx4 zero_piece = {0u, 0u, 0u, 0u};
+
+template <class T, Lie LIE, int ROWS, int BK, int WAVES>
+struct DirectOperand {
+    using E = typename View<T>::Element;
+    static constexpr int kParts_ = kParts<T>, kBytes = 2 * kParts_;           // of an element
+    static constexpr int kPerRow = (LIE == kAlong ? BK : ROWS) * kBytes / 16;   // pieces of a row in memory
+    static constexpr int kSize = ROWS * BK * kBytes;                          // bytes of a stage
+    static constexpr int kEach = kSize / 1024 / WAVES;                        // instructions of a wavefront per stage
+    static_assert(kEach * 1024 * WAVES == kSize && (LIE == kAcross || kPerRow == 8), "");
+    unsigned from[kEach];
+    __device__ __forceinline__ static int swizzle(int row) {
+        if constexpr (LIE == kAlong) return row >> 1 & 7;
+        else if constexpr (kParts_ == 2) return kPerRow >= 16 ? (row & 1) | (row & 2) << 2 : 0;
+        else return kPerRow >= 16 ? (row & 3) << 2 : kPerRow == 8 ? (row & 2) << 1 : 0;
+    }
+    __device__ __forceinline__ static int piece_index(int u) { return ((u * WAVES + (int)(threadIdx.x >> 6)) << 6) + (int)(threadIdx.x & 63); }
+    __device__ __forceinline__ static int row_of(int u) { return piece_index(u) / kPerRow; }
+    __device__ __forceinline__ static int piece_of(int u) { return piece_index(u) % kPerRow ^ swizzle(row_of(u)); }
+    __device__ __forceinline__ static int element_of(int u) { return piece_of(u) / kParts_ * 8; }      // the first of the piece's chunk
+
+    __device__ __forceinline__ void begin(const View<T>& x) {
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) {
+            int r = row_of(u), piece = piece_of(u);
+            if (LIE == kAlong && r >= x.rows) r = x.rows - 1;                  // rows past the end: any (their results are not stored)
+            if (LIE == kAcross && element_of(u) >= x.rows) piece = 0;          // (likewise)
+            from[u] = (unsigned)r * (unsigned)(x.ld * sizeof(E)) + piece * 16;
+        }
+    }
+    __device__ __forceinline__ void load(const View<T>& x, int64_t k0, char* S) const {
+        typedef const __attribute__((address_space(1))) void* Global;
+        typedef __attribute__((address_space(3))) void* Local;
+        const char* base = reinterpret_cast<const char*>(x.p) + (LIE == kAlong ? k0 * kBytes : k0 * x.ld * (int64_t)sizeof(E));
+        S += (threadIdx.x >> 6) * 1024;
+        const int64_t left = x.depth - k0;
+        if (left >= BK) {                                                     // (uniform)
+#pragma unroll
+            for (int u = 0; u < kEach; ++u) __builtin_amdgcn_global_load_lds((Global)(base + from[u]), (Local)(S + u * WAVES * 1024), 16, 0, 0);
+        } else {                                                              // what lies past the end of the contraction is zero
+#pragma unroll
+            for (int u = 0; u < kEach; ++u) {
+                const bool in = (LIE == kAlong ? element_of(u) : row_of(u)) < left;
+                const char* at = in ? base + from[u] : reinterpret_cast<const char*>(&zero_piece);
+                __builtin_amdgcn_global_load_lds((Global)at, (Local)(S + u * WAVES * 1024), 16, 0, 0);
+            }
+        }
+    }
+    // rows 32 b .. 32 b + 31, k 16 s .. 16 s + 15, part p, as the matrix cores take them
+    __device__ __forceinline__ static uintx4 operand(const char* S, int b, int s, int p) {
+        const int lane = threadIdx.x & 63;
+        if constexpr (LIE == kAlong) {
+            const int row = 32 * b + (lane & 31), piece = (2 * s + (lane >> 5)) * kParts_ + p;
+            return *reinterpret_cast<const uintx4*>(S + row * 128 + ((piece ^ swizzle(row)) << 4));
+        } else {
+            const int k = 16 * s + 8 * (lane >> 5) + ((lane & 15) >> 2), col = 32 * b + (lane & 16) + 4 * (lane & 3);
+            const char* from = S + (k * kPerRow + (((col >> 3) * kParts_ + p) ^ swizzle(k))) * 16 + (col & 4) * 2;
+            typedef __attribute__((address_space(3))) shortx4* Lds;
+            const shortx4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)from);
+            const shortx4 c = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(from + 4 * kPerRow * 16));        // (k + 4: the same permutation)
+            uintx4 v;
+            __builtin_memcpy(&v, &a, 8);
+            __builtin_memcpy(reinterpret_cast<char*>(&v) + 8, &c, 8);
+            return v;
+        }
+    }
+};
+
+template <class T, Lie XL, Lie YL, int WM_, int WN_, int TM_, int TN_, int STAGES_>
+struct Direct : Tile<WM_, WN_, TM_, TN_> {
+    using Base = Tile<WM_, WN_, TM_, TN_>;
+    using Base::WM; using Base::WN; using Base::TM; using Base::TN; using Base::BM; using Base::BN; using Base::THREADS; using Base::kSlabs;
+    static constexpr int P = kParts<T>, BK = 64 / P, SUBS = BK / 16, STAGES = STAGES_;
+    using X = DirectOperand<T, XL, BM, BK, WM * WN>;
+    using Y = DirectOperand<T, YL, BN, BK, WM * WN>;
+    static constexpr int kStage = X::kSize + Y::kSize;
+    static constexpr int kLds = STAGES * kStage / 2 > kSlabs ? STAGES * kStage / 2 : kSlabs;       // in 16-bit elements
+    static constexpr int kAhead = (STAGES - 2) * (X::kEach + Y::kEach);      // loads that may be on their way when the next step begins
+
+    struct Operands { uintx4 a[P][TM], b[P][TN]; };
+    __device__ __forceinline__ static void read(Operands& f, const char* S, int s) {
+        const int wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
+#pragma unroll
+        for (int p = P - 1; p >= 0; --p) {                                   // in the order of their use
+#pragma unroll
+            for (int j = 0; j < TN; ++j) f.b[P - 1 - p][j] = Y::operand(S + X::kSize, wn * TN + j, s, P - 1 - p);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) f.a[p][i] = X::operand(S, wm * TM + i, s, p);
+        }
+    }
+    __device__ __forceinline__ static void add(floatx16 (&acc)[TM][TN], const Operands& f) {
+        auto product = [&](int p, int q) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int i = 0; i < TM; ++i) acc[i][j] = multiply<T>(f.b[p][j], f.a[q][i], acc[i][j]);
+        };
+        if constexpr (P == 2) { product(0, 1); product(1, 0); }               // smallest terms first
+        product(0, 0);
+    }
+    // This wavefront's loads but for `ahead`, and its LDS reads, are done; then everybody's.
+    template <int AHEAD>
+    __device__ __forceinline__ static void meet() {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_s_waitcnt((AHEAD & 15) | 7 << 4 | (AHEAD >> 4) << 14);     // vmcnt(AHEAD) lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    }
+
+    __device__ __forceinline__ static void run(floatx16 (&acc)[TM][TN], const View<T>& x, const View<T>& y, unsigned short* lds) {
+        Base::clear(acc);
+        const int64_t depth = x.depth;
+        if (depth <= 0) return;
+        char* S = reinterpret_cast<char*>(lds);
+        X X_;
+        Y Y_;
+        X_.begin(x);
+        Y_.begin(y);
+#pragma unroll
+        for (int t = 0; t < STAGES - 1; ++t) {
+            X_.load(x, t * BK, S + t * kStage);
+            Y_.load(y, t * BK, S + t * kStage + X::kSize);
+        }
+        meet<kAhead>();
+        Operands f[2];
+        read(f[0], S, 0);
+        int now = 0, next = STAGES - 1;                                       // stages of this step and of the one loaded
+        for (int64_t k0 = 0; k0 < depth; k0 += BK) {
+            // into the stage of the step before, which nobody reads any more
+            X_.load(x, k0 + (STAGES - 1) * BK, S + next * kStage);
+            Y_.load(y, k0 + (STAGES - 1) * BK, S + next * kStage + X::kSize);
+#pragma unroll
+            for (int s = 0; s + 1 < SUBS; ++s) {
+                read(f[(s + 1) & 1], S + now * kStage, s + 1);
+                add(acc, f[s & 1]);
+            }
+            meet<kAhead>();
+            next = now;
+            now = now + 1 < STAGES ? now + 1 : 0;
+            read(f[0], S + now * kStage, 0);                                  // (after the last step: zeros)
+            add(acc, f[(SUBS - 1) & 1]);
+        }
+        meet<0>();                                                            // the LDS is free
+    }
 };
 
 // One quad of a row of `width` results at column c (c < width), the row at `to`; whole: width and the row's place are multiples of four
