@@ -507,13 +507,14 @@ struct Direct : Tile<WM_, WN_, TM_, TN_> {
         if constexpr (P == 2) { product(0, 1); product(1, 0); }               // smallest terms first
         product(0, 0);
     }
-    // This wavefront's loads but for `ahead`, and its LDS reads, are done; then everybody's.
+    // This wavefront's loads but for AHEAD, and its LDS reads, are done; then everybody's.  (The fences keep the compiler from moving
+    // accesses across; of a workgroup's scope, they would wait for all loads.)
     template <int AHEAD>
     __device__ __forceinline__ static void meet() {
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_s_waitcnt((AHEAD & 15) | 7 << 4 | (AHEAD >> 4) << 14);     // vmcnt(AHEAD) lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     }
 
     __device__ __forceinline__ static void run(floatx16 (&acc)[TM][TN], const View<T>& x, const View<T>& y, unsigned short* lds) {
