@@ -20,39 +20,68 @@ namespace {
 
 using namespace tile;
 
-constexpr int kNormBlocks = 64;        // most workgroups that add up one matrix's norm
+constexpr int kNormBlocks = 256;       // most workgroups that add up one matrix's norm
 
 // The direction of the update: the gradient, or what the momentum makes of it.
 template <class T>
 struct Source {
     const T* G; float* M; float mu; int nesterov;
-    __device__ __forceinline__ float first(int64_t e) const {             // with the momentum brought forward
-        const float g = (float)G[e];
-        if (!M) return g;
-        const float m = mu * M[e] + g;
-        M[e] = m;
-        return nesterov ? g + mu * m : m;
-    }
-    __device__ __forceinline__ float again(int64_t e) const {
-        if (!M) return (float)G[e];
-        const float m = M[e];
-        return nesterov ? (float)G[e] + mu * m : m;
-    }
+    __device__ __forceinline__ float direction(float g, float m) const { return nesterov ? g + mu * m : m; }
+    __device__ __forceinline__ float again(int64_t e) const { return M ? direction((float)G[e], M[e]) : (float)G[e]; }
 };
+
+// The sum of the squares of elements first, first + step, .. below count, with the momentum brought forward: sixteen loads are on their way
+// before the first is used.
+template <class T>
+__device__ __forceinline__ double squares(const Source<T>& src, int64_t base, int64_t first, int64_t step, int64_t count) {
+    constexpr int AHEAD = 8;
+    double sum = 0.0;
+    for (int64_t f = first; f < count; f += AHEAD * step) {
+        float g[AHEAD], m[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int64_t e = base + (f + u * step < count ? f + u * step : first);
+            g[u] = (float)src.G[e];
+            m[u] = src.M ? src.M[e] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            if (f + u * step >= count) continue;
+            float d = g[u];
+            if (src.M) {
+                const float now = src.mu * m[u] + g[u];
+                src.M[base + f + u * step] = now;
+                d = src.direction(g[u], now);
+            }
+            sum += (double)d * (double)d;
+        }
+    }
+    return sum;
+}
+
+// over a workgroup; everybody gets it
+template <int THREADS>
+__device__ __forceinline__ double block_sum(double sum, double* shared) {
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    sum = 0.0;
+    for (int i = 0; i < THREADS / 64; ++i) sum += shared[i];
+    return sum;
+}
+// What the direction is multiplied by, from its sum of squares: nothing where there is no direction (it is zero), and an entry
+// that is not finite leaves nothing finite.
+__device__ __forceinline__ double normaliser(double sum, float eps, float scale) {
+    const double norm = sqrt(sum) + (double)eps;
+    return norm == 0.0 ? 0.0 : norm < HUGE_VAL ? (double)scale / norm : __builtin_nan("");
+}
 
 template <class T>
 __global__ __launch_bounds__(256) void orthogonal_norm_kernel(Source<T> src, int64_t count, double* __restrict__ norms) {
-    const int64_t base = blockIdx.y * count;
-    __shared__ double sums[4];
-    double sum = 0.0;
-    for (int64_t f = (int64_t)blockIdx.x * 256 + threadIdx.x; f < count; f += (int64_t)gridDim.x * 256) {
-        const double d = src.first(base + f);
-        sum += d * d;
-    }
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) norms[blockIdx.y * kNormBlocks + blockIdx.x] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    __shared__ double shared[4];
+    const double sum = block_sum<256>(squares(src, blockIdx.y * count, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256, count), shared);
+    if (threadIdx.x == 0) norms[blockIdx.y * kNormBlocks + blockIdx.x] = sum;
 }
 
 __device__ __forceinline__ void split_pair(float x, _Float16& h, _Float16& l) {
@@ -85,20 +114,31 @@ struct Stack {
 template <class T>
 __global__ __launch_bounds__(256) void orthogonal_begin_kernel(Source<T> src, const double* __restrict__ norms, int n_norms, int K, int C,
                                                                float eps, float scale, Stack X) {
+    __shared__ double shared[4];
     const int64_t b = blockIdx.y;
-    double sum = 0.0;
-    for (int i = 0; i < n_norms; ++i) sum += norms[b * kNormBlocks + i];
-    const double norm = sqrt(sum) + (double)eps;
-    // (no direction: zero; an entry that is not finite: nothing is)
-    const double inv = norm == 0.0 ? 0.0 : norm < HUGE_VAL ? (double)scale / norm : __builtin_nan("");
+    const double inv = normaliser(block_sum<256>((int)threadIdx.x < n_norms ? norms[b * kNormBlocks + threadIdx.x] : 0.0, shared), eps, scale);
     const int quads = X.width / 4;
-    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < (int64_t)K * quads; q += (int64_t)gridDim.x * 256) {
-        const int64_t row = q / quads;
-        const int c = (int)(q % quads) * 4;
-        float v[4];
+    const int64_t most = (int64_t)K * quads;
+    for (int64_t q0 = (int64_t)blockIdx.x * 1024 + threadIdx.x; q0 < most; q0 += (int64_t)gridDim.x * 1024) {
+        float v[4][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = c + e < C ? (float)((double)src.again(b * K * C + row * C + c + e) * inv) : 0.f;
-        put_pair(X.matrix(b) + X.at((int)row, c), make_float4(v[0], v[1], v[2], v[3]));
+        for (int u = 0; u < 4; ++u) {
+            const int64_t q = q0 + 256 * u < most ? q0 + 256 * u : q0;
+            const int64_t row = q / quads;
+            const int c = (int)(q - row * quads) * 4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[u][e] = src.again(b * K * C + row * C + (c + e < C ? c + e : C - 1));
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int64_t q = q0 + 256 * u;
+            if (q >= most) continue;
+            const int64_t row = q / quads;
+            const int c = (int)(q - row * quads) * 4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[u][e] = c + e < C ? (float)((double)v[u][e] * inv) : 0.f;
+            put_pair(X.matrix(b) + X.at((int)row, c), make_float4(v[u][0], v[u][1], v[u][2], v[u][3]));
+        }
     }
 }
 
@@ -208,6 +248,231 @@ __global__ __launch_bounds__(P::THREADS, P::THREADS == 256 ? 2 : 1) void orthogo
     }
 }
 
+// Matrices with at most 32 RT (64 or 128) rows on the smaller side.  A workgroup of sixteen wavefronts holds X, that is a slab of up to
+// 16384 / RT / 32 of its columns, and S, then P, in LDS; with one slab the whole polynomial is one launch (256 x 64: fifteen products
+// in 95 us as launches of their own).  With more, a launch per step: every workgroup adds up the slabs' parts of S, forms P itself, applies
+// it to its slab and leaves its part of the next S.  X lies as its smaller side's rows, whichever way the matrix lies.
+constexpr int kMostSteps = 64;
+struct Schedule { float s[kMostSteps], p2[kMostSteps], p1[kMostSteps], p0[kMostSteps], x[kMostSteps]; };      // factors of S, S^2, S, 1 and of X' a step
+constexpr int kBlockX = 65536, kBlockS = 65536;          // bytes of LDS
+constexpr int kMostSlabs = 16;
+
+// A wavefront's operands from rows of PIECES pieces of 16 bytes in LDS (a chunk's eight high parts, its eight low ones); the pieces of a row are
+// permuted by its number so that both the sixteen rows that are read along it at once and the four that are read across hit different
+// banks.
+template <int PIECES>
+struct Rows {
+    __device__ __forceinline__ static int swizzle(int row) { return (row & 1) | (row & 2) << 2 | (row & 12) >> 1; }
+    __device__ __forceinline__ static int at(int row, int col) { return (row * PIECES + ((col >> 3 << 1) ^ swizzle(row))) * 16 + (col & 7) * 2; }       // high part; the low one: ^ 16
+    __device__ __forceinline__ static uintx4 along(const char* S, int b, int s, int p) {
+        const int lane = threadIdx.x & 63, row = 32 * b + (lane & 31), piece = (2 * s + (lane >> 5)) * 2 + p;
+        return *reinterpret_cast<const uintx4*>(S + (row * PIECES + (piece ^ swizzle(row))) * 16);
+    }
+    __device__ __forceinline__ static uintx4 across(const char* S, int b, int s, int p) {
+        typedef __attribute__((address_space(3))) shortx4* Lds;
+        const int lane = threadIdx.x & 63, k = 16 * s + 8 * (lane >> 5) + ((lane & 15) >> 2), col = 32 * b + (lane & 16) + 4 * (lane & 3);
+        const int piece = (col >> 3 << 1) + p, half = (col & 4) * 2;
+        const shortx4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(S + (k * PIECES + (piece ^ swizzle(k))) * 16 + half));
+        const shortx4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(S + ((k + 4) * PIECES + (piece ^ swizzle(k + 4))) * 16 + half));
+        uintx4 q;
+        __builtin_memcpy(&q, &u, 8);
+        __builtin_memcpy(reinterpret_cast<char*>(&q) + 8, &v, 8);
+        return q;
+    }
+    __device__ __forceinline__ static void put(char* S, int row, int col, float4 v) {
+        f16x4 h, l;
+        _Float16 a, b;
+        split_pair(v.x, a, b); h.x = a; l.x = b;
+        split_pair(v.y, a, b); h.y = a; l.y = b;
+        split_pair(v.z, a, b); h.z = a; l.z = b;
+        split_pair(v.w, a, b); h.w = a; l.w = b;
+        *reinterpret_cast<f16x4*>(S + at(row, col)) = h;
+        *reinterpret_cast<f16x4*>(S + (at(row, col) ^ 16)) = l;
+    }
+    // rows 32 bi .., columns 32 bj .. from a wavefront's accumulator (a row per lane, four columns in a row)
+    __device__ __forceinline__ static void put_tile(char* S, int bi, int bj, const floatx16& c) {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+            put(S, 32 * bi + (lane & 31), 32 * bj + 2 * r + 4 * (lane >> 5), make_float4(c[r], c[r + 1], c[r + 2], c[r + 3]));
+    }
+};
+__device__ __forceinline__ floatx16 multiply_pairs(const uintx4 (&y)[2], const uintx4 (&x)[2], floatx16 c) {
+    c = multiply<Pair>(y[0], x[1], c);
+    c = multiply<Pair>(y[1], x[0], c);
+    return multiply<Pair>(y[0], x[0], c);
+}
+
+// `one`: the whole polynomial (one slab); else step `step` of it, 0: only X and the first S.
+template <class T, int RT>
+__global__ __launch_bounds__(1024) void orthogonal_block_kernel(Source<T> src, const double* __restrict__ norms, int n_norms, int K, int C, float eps,
+                                                                float scale, int slabs, int one, int step, int steps, Schedule sch,
+                                                                char* __restrict__ images, float* __restrict__ parts_in, float* __restrict__ parts_out,
+                                                                T* __restrict__ out, float* __restrict__ W, float keep, float rate) {
+    constexpr int R = 32 * RT, WIDTH = kBlockX / 4 / R, CT = WIDTH / 32;         // rows, columns of the slab, tiles of 32 columns
+    constexpr int GROUPS = 16 / (RT * RT);                                   // wavefronts that share a tile of S
+    using XRows = Rows<WIDTH / 4>;
+    using SRows = Rows<R / 4>;
+    using Out = Tile<RT, 16 / RT, 1, 1>;
+    static_assert(CT * RT == 16 && Out::kSlabs * 2 <= kBlockX + kBlockS, "");
+    __shared__ __align__(256) char lds[kBlockX + kBlockS];
+    __shared__ double shared[16];
+    char* X = lds;
+    char* S = lds + kBlockX;                                                 // R * R * 4 bytes, behind it what is added up
+    float* sums = reinterpret_cast<float*>(S + R * R * 4);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t b = blockIdx.x / slabs;
+    const int slab = (int)(blockIdx.x % slabs);
+    const bool tall = K > C;
+    const int r = tall ? C : K, w = tall ? K : C, w0 = slab * WIDTH, ws = w - w0 < WIDTH ? w - w0 : WIDTH;
+    const int64_t base = b * K * C;
+
+    if (one || step == 0) {
+        const double sum = one ? squares(src, base, tid, 1024, (int64_t)K * C) : tid < n_norms ? norms[b * kNormBlocks + tid] : 0.0;
+        const double inv = normaliser(block_sum<1024>(sum, shared), eps, scale);      // (its barriers: M is what every thread has made it)
+        auto element = [&](int i, int j) {                                   // row i of the smaller side, column w0 + j
+            const bool in = i < r && j < ws;
+            const int64_t e = in ? tall ? (int64_t)(w0 + j) * C + i : (int64_t)i * C + w0 + j : 0;
+            const float d = src.again(base + e);
+            return in ? (float)((double)d * inv) : 0.f;
+        };
+        if (tall) {
+            // neighbouring threads take neighbouring elements in memory
+#pragma unroll 4
+            for (int f = tid; f < R * WIDTH; f += 1024) {
+                const int i = f % R, j = f / R;
+                _Float16* at = reinterpret_cast<_Float16*>(X + XRows::at(i, j));
+                _Float16* low = reinterpret_cast<_Float16*>(X + (XRows::at(i, j) ^ 16));
+                split_pair(element(i, j), *at, *low);
+            }
+        } else {
+#pragma unroll 4
+            for (int f = tid; f < R * WIDTH / 4; f += 1024) {
+                const int i = f / (WIDTH / 4), j = f % (WIDTH / 4) * 4;
+                XRows::put(X, i, j, make_float4(element(i, j), element(i, j + 1), element(i, j + 2), element(i, j + 3)));
+            }
+        }
+    } else {
+        const uintx4* from = reinterpret_cast<const uintx4*>(images + (int64_t)blockIdx.x * kBlockX);
+#pragma unroll
+        for (int f = 0; f < kBlockX / 16384; ++f) reinterpret_cast<uintx4*>(X)[tid + 1024 * f] = from[tid + 1024 * f];
+    }
+
+    const int tile = wave % (RT * RT), group = wave / (RT * RT), ti = tile / RT, tj = tile % RT;       // of S
+    const int xi = wave / CT, xj = wave % CT;                                                 // of X
+    floatx16 acc;
+    // (parts in the accumulators' order: 16 numbers of a lane, lanes of a tile, tiles)
+    auto load_sum = [&](const float* from) {
+        floatx16 v;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float4 f = *reinterpret_cast<const float4*>(from + (tile * 64 + lane) * 16 + 4 * q);
+            v[4 * q] = f.x; v[4 * q + 1] = f.y; v[4 * q + 2] = f.z; v[4 * q + 3] = f.w;
+        }
+        return v;
+    };
+    auto store_sum = [&](float* to, const floatx16& v) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) *reinterpret_cast<float4*>(to + (tile * 64 + lane) * 16 + 4 * q) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+    };
+    auto own_square = [&] {                                                    // this group's part of the slab's part of S
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+#pragma unroll
+        for (int t = 0; t < WIDTH / 16 / GROUPS; ++t) {
+            const int s = group * (WIDTH / 16 / GROUPS) + t;
+            const uintx4 x[2] = {XRows::along(X, ti, s, 0), XRows::along(X, ti, s, 1)}, y[2] = {XRows::along(X, tj, s, 0), XRows::along(X, tj, s, 1)};
+            acc = multiply_pairs(y, x, acc);
+        }
+    };
+    auto join_groups = [&] {                                                   // to group 0
+        if constexpr (GROUPS > 1) {
+            if (group > 0) store_sum(sums + (group - 1) * R * R, acc);
+            __syncthreads();
+            if (group == 0)
+#pragma unroll
+                for (int g = 1; g < GROUPS; ++g) acc += load_sum(sums + (g - 1) * R * R);
+        }
+    };
+    auto leave_part = [&] {
+        own_square();
+        join_groups();
+        if (group == 0) store_sum(parts_out + (int64_t)blockIdx.x * R * R, acc);
+    };
+
+    if (!one && step == 0) leave_part();
+    for (int k = one ? 0 : step > 0 ? step - 1 : 0; k < (one ? steps : step); ++k) {
+        if (one) own_square();
+        else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+#pragma unroll 2
+            for (int t = group; t < slabs; t += GROUPS) acc += load_sum(parts_in + (b * slabs + t) * R * R);
+            __syncthreads();                                                 // (X is there)
+        }
+        join_groups();
+        floatx16 square;
+        if (group == 0) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[e] *= sch.s[k];
+            SRows::put_tile(S, ti, tj, acc);
+        }
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) square[e] = 0.f;
+#pragma unroll
+            for (int s = 0; s < R / 16; ++s) {
+                const uintx4 x[2] = {SRows::along(S, ti, s, 0), SRows::along(S, ti, s, 1)}, y[2] = {SRows::along(S, tj, s, 0), SRows::along(S, tj, s, 1)};
+                square = multiply_pairs(y, x, square);
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int col = 32 * tj + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
+                square[e] = sch.p2[k] * square[e] + sch.p1[k] * acc[e] + (col == 32 * ti + (lane & 31) ? sch.p0[k] : 0.f);
+            }
+        }
+        __syncthreads();
+        if (group == 0) SRows::put_tile(S, ti, tj, square);
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+#pragma unroll
+        for (int s = 0; s < R / 16; ++s) {
+            const uintx4 x[2] = {SRows::along(S, xi, s, 0), SRows::along(S, xi, s, 1)}, y[2] = {XRows::across(X, xj, s, 0), XRows::across(X, xj, s, 1)};
+            acc = multiply_pairs(y, x, acc);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[e] *= sch.x[k];
+        __syncthreads();                                                     // (nobody reads the old X any more)
+        if (k + 1 < steps) XRows::put_tile(X, xi, xj, acc);
+    }
+    if (!one && step < steps) {
+        if (step > 0) leave_part();
+        else __syncthreads();
+        uintx4* to = reinterpret_cast<uintx4*>(images + (int64_t)blockIdx.x * kBlockX);
+#pragma unroll
+        for (int f = 0; f < kBlockX / 16384; ++f) to[tid + 1024 * f] = reinterpret_cast<const uintx4*>(X)[tid + 1024 * f];
+        return;
+    }
+    floatx16 last[1][1] = {{acc}};
+    auto store = [&](int row, int col, float4 v) {                             // four elements of a row of the matrix
+        if (row >= K || col >= C) return;
+        const float q[4] = {v.x, v.y, v.z, v.w};
+        const int64_t at = base + (int64_t)row * C + col;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (col + e >= C) continue;
+            if (W) W[at + e] = keep * W[at + e] - rate * q[e];
+            else out[at + e] = (T)q[e];
+        }
+    };
+    if (tall) Out::template drain<true>(last, reinterpret_cast<unsigned short*>(lds), [](int, int, float4 v) { return v; },
+                                        [&](int col, int row, float4 v) { if (col < ws) store(w0 + col, row, v); });
+    else Out::drain(last, reinterpret_cast<unsigned short*>(lds), [&](int row, int col, float4 v) { store(row, w0 + col, v); });
+}
+
 template <Lie X, Lie Y> using Large = Direct<Pair, X, Y, 2, 4, 4, 2, 2>;         // 256 x 256
 template <Lie X, Lie Y> using Middle = Direct<Pair, X, Y, 2, 2, 2, 2, 2>;        // 128 x 128
 template <Lie X, Lie Y> using Small = Direct<Pair, X, Y, 2, 2, 1, 1, 4>;         // 64 x 64
@@ -265,14 +530,62 @@ const char* orthogonal_fault(int batch, int K, int C) {
 }
 
 namespace {
-struct Layout { int64_t x, s, bytes; };               // elements of X and of S, and bytes of everything
-Layout layout(int64_t batch, int64_t K, int64_t C) {
+// Rows of 32 on the smaller side that a workgroup holds in LDS, and slabs of columns; 0: it does not.
+struct Blocks { int rt, slabs; };
+Blocks blocks_of(int K, int C) {
+    const int r = std::min(K, C), w = std::max(K, C), rt = r <= 64 ? 2 : 4;
+    const int64_t slabs = over(w, kBlockX / 4 / 32 / rt);
+    return r <= 128 && slabs <= kMostSlabs ? Blocks{rt, (int)slabs} : Blocks{0, 0};
+}
+struct Layout { int64_t x, s, parts, bytes; };         // elements of X and of S, floats of the slabs' parts of S, and bytes of everything
+Layout layout(int64_t batch, int K, int C) {
     const int64_t r = std::min(K, C);
-    Layout l;
-    l.x = batch * K * row_pairs(C);
-    l.s = batch * r * row_pairs(r);
-    l.bytes = 8 * kNormBlocks * batch + 2 * (2 * 2 * l.x + 2 * 2 * l.s) + 5 * 256;
+    const Blocks bl = blocks_of(K, C);
+    Layout l{0, 0, 0, 8 * kNormBlocks * batch + 5 * 256};
+    if (bl.rt) {
+        l.parts = batch * bl.slabs * (32 * bl.rt) * (32 * bl.rt);
+        if (bl.slabs > 1) l.bytes += batch * bl.slabs * kBlockX + 2 * 4 * l.parts;
+    } else {
+        l.x = batch * K * row_pairs(C);
+        l.s = batch * r * row_pairs(r);
+        l.bytes += 4 * (2 * l.x + 2 * l.s);
+    }
     return l;
+}
+
+// Powers of two that X, S and P carry, step by step.
+struct Scales { int x, s, p, next; };
+struct Bounds {
+    double a, b, c, bound = 1.0;
+    Scales step() {
+        const double s2 = bound * bound, vertex = c != 0.0 ? -b / (2.0 * c) : -1.0;
+        auto p = [&](double x) { return std::fabs(a + x * (b + c * x)); };
+        double most = std::max(p(0.0), p(s2));
+        if (vertex > 0.0 && vertex < s2) most = std::max(most, p(vertex));
+        Scales e{scale_for(bound), scale_for(s2), scale_for(most), 0};
+        bound = polynomial_bound(a, b, c, bound);
+        e.next = scale_for(bound);
+        return e;
+    }
+};
+
+template <class T, int RT>
+void launch_blocks(hipStream_t s, const Orthogonal& a, const Source<T>& src, int slabs, double* norms, int n_norms, char* images, float* parts, int64_t part_floats) {
+    Schedule sch;
+    Bounds bounds{a.a, a.b, a.c};
+    for (int k = 0; k < a.steps; ++k) {
+        const Scales e = bounds.step();
+        sch.s[k] = std::ldexp(1.f, e.s - 2 * e.x);
+        sch.p2[k] = (float)std::ldexp((double)a.c, e.p - 2 * e.s);
+        sch.p1[k] = (float)std::ldexp((double)a.b, e.p - e.s);
+        sch.p0[k] = (float)std::ldexp((double)a.a, e.p);
+        sch.x[k] = std::ldexp(1.f, (k + 1 == a.steps ? 0 : e.next) - e.p - e.x);
+    }
+    const float scale = std::ldexp(1.f, scale_for(1.0));
+    for (int step = slabs > 1 ? 0 : a.steps; step <= a.steps; ++step)
+        orthogonal_block_kernel<T, RT><<<dim3((unsigned)(a.batch * slabs)), dim3(1024), 0, s>>>(
+            src, norms, n_norms, a.K, a.C, a.eps, scale, slabs, slabs == 1, step, a.steps, sch, images, parts + (step + 1) % 2 * part_floats,
+            parts + step % 2 * part_floats, (T*)a.out, a.W, a.keep, a.rate);
 }
 }  // namespace
 
@@ -282,36 +595,41 @@ void launch_orthogonalise(hipStream_t s, int type, const Orthogonal& a) {
     const int r = std::min(a.K, a.C), w = std::max(a.K, a.C), ld = (int)row_pairs(a.C), lds = (int)row_pairs(r);
     const bool wide = a.K <= a.C;
     const Layout l = layout(a.batch, a.K, a.C);
+    const Blocks bl = blocks_of(a.K, a.C);
     char* at = (char*)a.scratch;
     auto take = [&](int64_t bytes) { char* p = at; at += over(bytes, 256) * 256; return p; };
     double* norms = (double*)take(8 * kNormBlocks * (int64_t)a.batch);
-    Stack X{(_Float16*)take(4 * l.x), (int64_t)2 * a.K * ld, ld, (int)round8(a.C)}, Y{(_Float16*)take(4 * l.x), (int64_t)2 * a.K * ld, ld, (int)round8(a.C)};
-    Stack S{(_Float16*)take(4 * l.s), (int64_t)2 * r * lds, lds, (int)round8(r)}, Q{(_Float16*)take(4 * l.s), (int64_t)2 * r * lds, lds, (int)round8(r)};
-
-    double bound = 1.0;
-    int ex = scale_for(bound);
     const int64_t count = (int64_t)a.K * a.C;
-    auto begin = [&](auto* t) {
+    const int nb = (int)std::min<int64_t>(over(count, 2048), kNormBlocks);
+    auto typed = [&](auto f) {
+        if (type == kBf16) f((__bf16*)nullptr);
+        else if (type == kF16) f((_Float16*)nullptr);
+        else f((float*)nullptr);
+    };
+    typed([&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
         const Source<T> src{(const T*)a.G, a.M, a.mu, a.nesterov};
-        const int nb = (int)std::min<int64_t>(over(count, 1024), kNormBlocks);
-        orthogonal_norm_kernel<T><<<dim3(nb, a.batch), dim3(256), 0, s>>>(src, count, norms);
-        orthogonal_begin_kernel<T><<<dim3((unsigned)std::min<int64_t>(over(a.K * (round8(a.C) / 4), 256), 1024), a.batch), dim3(256), 0, s>>>(
-            src, norms, nb, a.K, a.C, a.eps, std::ldexp(1.f, ex), X);
-    };
-    if (type == kBf16) begin((__bf16*)nullptr);
-    else if (type == kF16) begin((_Float16*)nullptr);
-    else begin((float*)nullptr);
+        if (bl.slabs != 1) orthogonal_norm_kernel<T><<<dim3(nb, a.batch), dim3(256), 0, s>>>(src, count, norms);
+        if (!bl.rt) return;
+        char* images = take(bl.slabs > 1 ? (int64_t)a.batch * bl.slabs * kBlockX : 0);
+        float* parts = (float*)take(bl.slabs > 1 ? 2 * 4 * l.parts : 0);
+        if (bl.rt == 2) launch_blocks<T, 2>(s, a, src, bl.slabs, norms, nb, images, parts, l.parts);
+        else launch_blocks<T, 4>(s, a, src, bl.slabs, norms, nb, images, parts, l.parts);
+    });
+    if (bl.rt) return;
+
+    Stack X{(_Float16*)take(4 * l.x), (int64_t)2 * a.K * ld, ld, (int)round8(a.C)}, Y{(_Float16*)take(4 * l.x), (int64_t)2 * a.K * ld, ld, (int)round8(a.C)};
+    Stack S{(_Float16*)take(4 * l.s), (int64_t)2 * r * lds, lds, (int)round8(r)}, Q{(_Float16*)take(4 * l.s), (int64_t)2 * r * lds, lds, (int)round8(r)};
+    typed([&](auto* t) {
+        using T = std::remove_pointer_t<decltype(t)>;
+        orthogonal_begin_kernel<T><<<dim3((unsigned)std::min<int64_t>(over(a.K * (round8(a.C) / 4), 1024), 1024), a.batch), dim3(256), 0, s>>>(
+            Source<T>{(const T*)a.G, a.M, a.mu, a.nesterov}, norms, nb, a.K, a.C, a.eps, std::ldexp(1.f, scale_for(1.0)), X);
+    });
 
     const Size square = size_of(a.batch, r, r, true), apply = size_of(a.batch, a.K, a.C, false);
+    Bounds bounds{a.a, a.b, a.c};
     for (int k = 0; k < a.steps; ++k) {
-        const double s2 = bound * bound, vertex = a.c != 0.f ? -(double)a.b / (2.0 * a.c) : -1.0;
-        auto p = [&](double x) { return std::fabs(a.a + x * (a.b + (double)a.c * x)); };
-        double most = std::max(p(0.0), p(s2));
-        if (vertex > 0.0 && vertex < s2) most = std::max(most, p(vertex));
-        const int es = scale_for(s2), ep = scale_for(most);
-        bound = polynomial_bound(a.a, a.b, a.c, bound);
-        const int en = scale_for(bound);
+        const auto [ex, es, ep, en] = bounds.step();
         const bool last = k + 1 == a.steps;
         with_size(square, [&](auto size) {
             const int tr = (int)over(r, kSizeRows[size]), tc = (int)over(r, kSizeCols[size]);
@@ -342,7 +660,6 @@ void launch_orthogonalise(hipStream_t s, int type, const Orthogonal& a) {
             else go((_Float16*)nullptr);
         });
         std::swap(X, Y);
-        ex = en;
     }
 }
 

@@ -66,7 +66,7 @@ def gradient(torch, seed, batch, K, width, kind, scale=1e-3):
 
 SHAPES = [(1, 1, 1), (1, 1, 7), (1, 5, 1), (3, 2, 2), (2, 16, 16), (1, 64, 64), (2, 33, 65), (1, 256, 64), (3, 64, 256), (1, 97, 301), (2, 128, 128),
           (1, 130, 129), (1, 256, 256), (5, 100, 40), (1, 767, 1000), (1, 1000, 10), (2, 300, 700), (1, 512, 512), (40, 12, 20), (1, 3, 2500), (1, 640, 130),
-          (2, 192, 2048)]
+          (2, 192, 2048), (3, 64, 257), (2, 700, 33), (1, 128, 129), (2, 100, 2048), (1, 2049, 128), (1, 4096, 64), (1, 4100, 20), (2, 65, 640)]
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
