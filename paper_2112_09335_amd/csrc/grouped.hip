@@ -142,33 +142,48 @@ void with_type(int type, F f) {
     else f((float*)nullptr);
 }
 
-// Tiles (wavefronts, 32 x 32 accumulators of one, contraction per step, steps ahead, LDS buffers).  Large ones read each operand from LDS
-// once for 128 x 256 results, two workgroups a compute unit; the small ones are for products that would not fill the chip with them.
+// Tiles: wavefronts, 32 x 32 accumulators of one; then, through registers, contraction per step, steps ahead, LDS buffers, or, straight to
+// LDS, stages.  Large ones read each operand from LDS once for 128 x 256 results, two workgroups a compute unit, or for 256 x 256,
+// one; the small ones are for products that would not fill the chip with them.
 template <class T> constexpr int kStep = 128 / sizeof(T);
-template <class T, Lie X, Lie Y, Mode M> using Large = Product<T, X, Y, M, 2, 2, 2, 4, X == kAlong ? kStep<T> : kStep<T> / 2, 1, 1>;          // 128 x 256
-template <class T, Lie X, Lie Y, Mode M> using Middle = Product<T, X, Y, M, 2, 2, 2, 2, kStep<T>, 1, 1>;         // 128 x 128
-template <class T, Lie X, Lie Y, Mode M> using Small = Product<T, X, Y, M, 2, 2, 1, 1, kStep<T>, 2, 2>;          // 64 x 64
-template <class T, Lie X, Lie Y, Mode M> using Few = Product<T, X, Y, M, 1, 2, 1, 1, kStep<T>, 4, 2>;            // 32 x 64
-
 enum Size { kLarge, kMiddle, kSmall, kFew };
-constexpr int kSizeRows[] = {128, 128, 64, 32}, kSizeCols[] = {256, 128, 64, 64};
+template <class T, Lie X, Lie Y, Mode M, bool STRAIGHT = sizeof(T) == 2 && M == kWhole>
+struct Sizes {
+    using Large = Product<T, X, Y, M, 2, 2, 2, 4, X == kAlong ? kStep<T> : kStep<T> / 2, 1, 1>;          // 128 x 256
+    using Middle = Product<T, X, Y, M, 2, 2, 2, 2, kStep<T>, 1, 1>;                                   // 128 x 128
+    using Small = Product<T, X, Y, M, 2, 2, 1, 1, kStep<T>, 2, 2>;                                    // 64 x 64
+    using Few = Product<T, X, Y, M, 1, 2, 1, 1, kStep<T>, 4, 2>;                                      // 32 x 64
+};
+template <class T, Lie X, Lie Y, Mode M>
+struct Sizes<T, X, Y, M, true> {
+    using Large = Direct<T, X, Y, 2, 4, 4, 2, 2>;              // 256 x 256
+    using Middle = Direct<T, X, Y, 2, 2, 2, 2, 2>;             // 128 x 128
+    using Small = Direct<T, X, Y, 2, 2, 1, 1, 4>;              // 64 x 64
+    using Few = Direct<T, X, Y, 1, 2, 1, 1, 6>;                // 32 x 64
+};
+template <Size SIZE, class T, Lie X, Lie Y, Mode M>
+using Sized = std::conditional_t<SIZE == kLarge, typename Sizes<T, X, Y, M>::Large, std::conditional_t<SIZE == kMiddle, typename Sizes<T, X, Y, M>::Middle,
+              std::conditional_t<SIZE == kSmall, typename Sizes<T, X, Y, M>::Small, typename Sizes<T, X, Y, M>::Few>>>;
+constexpr int kSizeCols[] = {256, 128, 64, 64};
+int size_rows(Size s, bool straight) { return s == kLarge ? straight ? 256 : 128 : s == kMiddle ? 128 : s == kSmall ? 64 : 32; }
 constexpr int64_t kCus = 256;
 
 int64_t over(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-Size nn_size(int64_t n, int C, int groups) {
+Size nn_size(int64_t n, int C, int groups, bool straight) {
     const int64_t hit = std::min<int64_t>(n, groups), rows = over(n, hit);            // rows of a group that has any, if they share alike
     for (Size s : {kLarge, kMiddle, kSmall}) {
-        const bool fits = C > kSizeCols[s] / 2 && rows > kSizeRows[s] / 2;
-        if (fits && (n / kSizeRows[s] + hit / 2) * over(C, kSizeCols[s]) >= kCus) return s;
+        const int r = size_rows(s, straight);
+        const bool fits = C > kSizeCols[s] / 2 && rows > r / 2;
+        if (fits && (n / r + hit / 2) * over(C, kSizeCols[s]) >= kCus) return s;
     }
     return rows > 32 ? kSmall : kFew;
 }
 
 struct TnPlan { Size size; int64_t most, parts; };
-TnPlan tn_plan(int64_t n, int K, int C, int groups) {
-    const Size s = K > 64 && C > 128 ? kLarge : K > 64 && C > 64 ? kMiddle : kSmall;
-    const int64_t tiles = over(K, kSizeRows[s]) * over(C, kSizeCols[s]);
+TnPlan tn_plan(int64_t n, int K, int C, int groups, bool straight) {
+    const Size s = K > size_rows(kLarge, straight) / 2 && C > 128 ? kLarge : K > 64 && C > 64 ? kMiddle : kSmall;
+    const int64_t tiles = over(K, size_rows(s, straight)) * over(C, kSizeCols[s]);
     TnPlan p{s, n > 0 ? n : 1, 0};
     // too few tiles for two workgroups a compute unit: the rows are shared out too, 256 of them at least
     if (tiles * groups < 2 * kCus * 2) p.most = std::max<int64_t>(256, over(over(n * tiles, 2 * kCus), 64) * 64);
@@ -178,10 +193,6 @@ TnPlan tn_plan(int64_t n, int K, int C, int groups) {
 int64_t part_floats(int K, int C) { return over((int64_t)K * C, 4) * 4; }
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-
-template <Size SIZE, class T, Lie X, Lie Y, Mode M>
-using Sized = std::conditional_t<SIZE == kLarge, Large<T, X, Y, M>, std::conditional_t<SIZE == kMiddle, Middle<T, X, Y, M>,
-              std::conditional_t<SIZE == kSmall, Small<T, X, Y, M>, Few<T, X, Y, M>>>>;
 
 template <class T, Lie YL, Mode MODE>
 void nn_launch(hipStream_t s, const GroupedNN& a, Size size, bool whole_out) {
@@ -223,25 +234,36 @@ void tn_launch(hipStream_t s, const GroupedTN& a, const TnPlan& plan) {
 
 }  // namespace
 
+// (whole chunks can go straight to LDS, or not: the most workgroups of either, and the scratch that serves both)
 int64_t grouped_nn_blocks(int64_t n, int C, int groups) {
-    if (n == 0) return 0;
-    const Size s = nn_size(n, C, groups);
-    return (n / kSizeRows[s] + groups) * over(C, kSizeCols[s]);
+    int64_t most = 0;
+    for (bool straight : {false, true}) {
+        if (n == 0) continue;
+        const Size s = nn_size(n, C, groups, straight);
+        most = std::max(most, (n / size_rows(s, straight) + groups) * over(C, kSizeCols[s]));
+    }
+    return most;
 }
 int64_t grouped_tn_blocks(int64_t n, int K, int C, int groups) {
-    const TnPlan p = tn_plan(n, K, C, groups);
-    return (n / p.most + groups) * over(K, kSizeRows[p.size]) * over(C, kSizeCols[p.size]);
+    int64_t most = 0;
+    for (bool straight : {false, true}) {
+        const TnPlan p = tn_plan(n, K, C, groups, straight);
+        most = std::max(most, (n / p.most + groups) * over(K, size_rows(p.size, straight)) * over(C, kSizeCols[p.size]));
+    }
+    return most;
 }
-size_t grouped_tn_scratch(int64_t n, int K, int C, int groups) { return sizeof(float) * tn_plan(n, K, C, groups).parts * part_floats(K, C); }
+size_t grouped_tn_scratch(int64_t n, int K, int C, int groups) {
+    return sizeof(float) * std::max(tn_plan(n, K, C, groups, false).parts, tn_plan(n, K, C, groups, true).parts) * part_floats(K, C);
+}
 
 void launch_grouped_nn(hipStream_t s, int type, const GroupedNN& a) {
     if (a.n == 0) return;
-    const Size size = nn_size(a.n, a.C, a.groups);
     with_type(type, [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
         constexpr int64_t Q = 16 / sizeof(T);
         const bool whole = a.K % 8 == 0 && a.lda % Q == 0 && aligned16(a.A) && aligned16(a.B) && a.lda * (int64_t)sizeof(T) <= kMostRow && (a.transposed || a.C % 8 == 0);
         const bool whole_out = a.C % 4 == 0 && a.ldo % 4 == 0 && ((uintptr_t)a.out & (4 * sizeof(T) - 1)) == 0;
+        const Size size = nn_size(a.n, a.C, a.groups, whole && sizeof(T) == 2);
         if (a.transposed) {
             if (whole) nn_launch<T, kAlong, kWhole>(s, a, size, whole_out);
             else nn_launch<T, kAlong, kAny>(s, a, size, whole_out);
@@ -253,12 +275,12 @@ void launch_grouped_nn(hipStream_t s, int type, const GroupedNN& a) {
 }
 
 void launch_grouped_tn(hipStream_t s, int type, int out_type, const GroupedTN& a) {
-    const TnPlan plan = tn_plan(a.n, a.K, a.C, a.groups);
     with_type(type, [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
         constexpr int64_t Q = 16 / sizeof(T);
         const bool whole = a.K % 8 == 0 && a.C % 8 == 0 && a.lda % Q == 0 && a.ldg % Q == 0 && aligned16(a.A) && aligned16(a.G) &&
                            std::max(a.lda, a.ldg) * (int64_t)sizeof(T) <= kMostRow;
+        const TnPlan plan = tn_plan(a.n, a.K, a.C, a.groups, whole && sizeof(T) == 2);
         auto go = [&](auto* o) {
             using O = std::remove_pointer_t<decltype(o)>;
             if (whole) tn_launch<T, kWhole, O>(s, a, plan);

@@ -475,11 +475,13 @@ __global__ __launch_bounds__(1024) void orthogonal_block_kernel(Source<T> src, c
 
 template <Lie X, Lie Y> using Large = Direct<Pair, X, Y, 2, 4, 4, 2, 2>;         // 256 x 256
 template <Lie X, Lie Y> using Middle = Direct<Pair, X, Y, 2, 2, 2, 2, 2>;        // 128 x 128
-template <Lie X, Lie Y> using Small = Direct<Pair, X, Y, 2, 2, 1, 1, 4>;         // 64 x 64
-enum Size { kLarge, kMiddle, kSmall };
-constexpr int kSizeRows[] = {256, 128, 64}, kSizeCols[] = {256, 128, 64};
+template <Lie X, Lie Y> using Small = Direct<Pair, X, Y, 2, 2, 1, 1, 2, 2>;      // 64 x 64, two workgroups a compute unit
+template <Lie X, Lie Y> using Lone = Direct<Pair, X, Y, 2, 2, 1, 1, 2, 4>;       // 64 x 64, one
+enum Size { kLarge, kMiddle, kSmall, kLone };
+constexpr int kSizeRows[] = {256, 128, 64, 64}, kSizeCols[] = {256, 128, 64, 64};
 template <Size SIZE, Lie X, Lie Y>
-using Sized = std::conditional_t<SIZE == kLarge, Large<X, Y>, std::conditional_t<SIZE == kMiddle, Middle<X, Y>, Small<X, Y>>>;
+using Sized = std::conditional_t<SIZE == kLarge, Large<X, Y>, std::conditional_t<SIZE == kMiddle, Middle<X, Y>,
+              std::conditional_t<SIZE == kSmall, Small<X, Y>, Lone<X, Y>>>>;
 
 int64_t over(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t round8(int64_t n) { return (n + 7) / 8 * 8; }
@@ -491,13 +493,14 @@ constexpr int64_t kCus = 256;
 Size size_of(int64_t batch, int64_t rows, int64_t cols, bool half) {
     for (Size s : {kLarge, kMiddle})
         if (batch * over(rows, kSizeRows[s]) * over(cols, kSizeCols[s]) >= (half ? 2 : 1) * kCus) return s;
-    return kSmall;
+    return batch * over(rows, 64) * over(cols, 64) > (half ? 2 : 1) * kCus ? kSmall : kLone;
 }
 template <class F>
 void with_size(Size s, F f) {
     if (s == kLarge) f(std::integral_constant<Size, kLarge>());
     else if (s == kMiddle) f(std::integral_constant<Size, kMiddle>());
-    else f(std::integral_constant<Size, kSmall>());
+    else if (s == kSmall) f(std::integral_constant<Size, kSmall>());
+    else f(std::integral_constant<Size, kLone>());
 }
 
 // The power of two that brings `most` to 2^13 .. 2^14 (of what is far below one, less near).

@@ -256,10 +256,11 @@ __device__ __forceinline__ floatx16 multiply(uintx4 a, uintx4 b, floatx16 c) {
 }
 
 // What tiles of WM x WN wavefronts, TM x TN accumulators of 32 x 32 each, have in common.
-template <int WM_, int WN_, int TM_, int TN_>
+// WK: as many sets of WM x WN wavefronts share the steps of the contraction; the first set gets the results.
+template <int WM_, int WN_, int TM_, int TN_, int WK_ = 1>
 struct Tile {
-    static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_;
-    static constexpr int BM = 32 * TM * WM, BN = 32 * TN * WN, THREADS = 64 * WM * WN;
+    static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, WK = WK_;
+    static constexpr int BM = 32 * TM * WM, BN = 32 * TN * WN, THREADS = 64 * WM * WN * WK;
     // results on their way out: 32 rows by up to 64 columns of a wavefront, at a time
     static constexpr int kSlabCols = TN >= 2 ? 64 : 32, kSlabLd = kSlabCols + 4;
     static constexpr int kSlabs = WM * WN * 32 * kSlabLd * 2;            // in 16-bit elements
@@ -279,6 +280,7 @@ struct Tile {
     __device__ __forceinline__ static void drain(floatx16 (&acc)[TM][TN], unsigned short* S, F f, M m) {
         constexpr int J = kSlabCols / 32, Q = kSlabCols / 4;
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
+        if (wave >= WM * WN) return;
         float* C = reinterpret_cast<float*>(S) + wave * 32 * kSlabLd;
         auto settled = [] {                                             // a wavefront's LDS accesses are done in their order
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -297,7 +299,8 @@ struct Tile {
                         *reinterpret_cast<float4*>(C + (lane & 31) * kSlabLd + 32 * j + 2 * r + 4 * (lane >> 5)) =
                             make_float4(acc[i][j0 + j][r], acc[i][j0 + j][r + 1], acc[i][j0 + j][r + 2], acc[i][j0 + j][r + 3]);
                 settled();
-#pragma unroll
+                // (rolled up: this code runs once a workgroup, and is fetched for it)
+#pragma unroll 2
                 for (int u = 0; u < 32 * Q / 64; ++u) {
                     const int row = (lane + 64 * u) / Q, col = (lane + 64 * u) % Q * 4;
                     float4* at = reinterpret_cast<float4*>(C + row * kSlabLd + col);
@@ -306,7 +309,7 @@ struct Tile {
                 }
                 if constexpr (MIRROR) {
                     settled();
-#pragma unroll
+#pragma unroll 1
                     for (int u = 0; u < 32 * Q / 64; ++u) {
                         const int row = lane % 8 * 4, col = lane / 8 + 8 * u;
                         const float* at = C + row * kSlabLd + col;
@@ -423,7 +426,8 @@ struct DirectOperand {
         else if constexpr (kParts_ == 2) return kPerRow >= 16 ? (row & 1) | (row & 2) << 2 : 0;
         else return kPerRow >= 16 ? (row & 3) << 2 : kPerRow == 8 ? (row & 2) << 1 : 0;
     }
-    __device__ __forceinline__ static int piece_index(int u) { return ((u * WAVES + (int)(threadIdx.x >> 6)) << 6) + (int)(threadIdx.x & 63); }
+    __device__ __forceinline__ static int wave() { return (threadIdx.x >> 6) % WAVES; }
+    __device__ __forceinline__ static int piece_index(int u) { return ((u * WAVES + wave()) << 6) + (int)(threadIdx.x & 63); }
     __device__ __forceinline__ static int row_of(int u) { return piece_index(u) / kPerRow; }
     __device__ __forceinline__ static int piece_of(int u) { return piece_index(u) % kPerRow ^ swizzle(row_of(u)); }
     __device__ __forceinline__ static int element_of(int u) { return piece_of(u) / kParts_ * 8; }      // the first of the piece's chunk
@@ -441,7 +445,7 @@ struct DirectOperand {
         typedef const __attribute__((address_space(1))) void* Global;
         typedef __attribute__((address_space(3))) void* Local;
         const char* base = reinterpret_cast<const char*>(x.p) + (LIE == kAlong ? k0 * kBytes : k0 * x.ld * (int64_t)sizeof(E));
-        S += (threadIdx.x >> 6) * 1024;
+        S += __builtin_amdgcn_readfirstlane(wave()) * 1024;
         const int64_t left = x.depth - k0;
         if (left >= BK) {                                                     // (uniform)
 #pragma unroll
@@ -475,20 +479,22 @@ struct DirectOperand {
     }
 };
 
-template <class T, Lie XL, Lie YL, int WM_, int WN_, int TM_, int TN_, int STAGES_>
-struct Direct : Tile<WM_, WN_, TM_, TN_> {
-    using Base = Tile<WM_, WN_, TM_, TN_>;
-    using Base::WM; using Base::WN; using Base::TM; using Base::TN; using Base::BM; using Base::BN; using Base::THREADS; using Base::kSlabs;
+template <class T, Lie XL, Lie YL, int WM_, int WN_, int TM_, int TN_, int STAGES_, int WK_ = 1>
+struct Direct : Tile<WM_, WN_, TM_, TN_, WK_> {
+    using Base = Tile<WM_, WN_, TM_, TN_, WK_>;
+    using Base::WM; using Base::WN; using Base::TM; using Base::TN; using Base::WK; using Base::BM; using Base::BN; using Base::THREADS; using Base::kSlabs;
     static constexpr int P = kParts<T>, BK = 64 / P, SUBS = BK / 16, STAGES = STAGES_;
     using X = DirectOperand<T, XL, BM, BK, WM * WN>;
     using Y = DirectOperand<T, YL, BN, BK, WM * WN>;
     static constexpr int kStage = X::kSize + Y::kSize;
-    static constexpr int kLds = STAGES * kStage / 2 > kSlabs ? STAGES * kStage / 2 : kSlabs;       // in 16-bit elements
+    static constexpr int kSet = STAGES * kStage;                              // bytes of a set of wavefronts
+    static constexpr int kSums = (WK - 1) * BM * BN * 4 + 2 * kSlabs;          // what the sets leave each other, behind the slabs
+    static constexpr int kLds = (WK * kSet > kSums ? WK * kSet : kSums) / 2;     // in 16-bit elements
     static constexpr int kAhead = (STAGES - 2) * (X::kEach + Y::kEach);      // loads that may be on their way when the next step begins
 
     struct Operands { uintx4 a[P][TM], b[P][TN]; };
     __device__ __forceinline__ static void read(Operands& f, const char* S, int s) {
-        const int wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
+        const int wave = (threadIdx.x >> 6) % (WM * WN), wm = wave / WN, wn = wave % WN;
 #pragma unroll
         for (int p = P - 1; p >= 0; --p) {                                   // in the order of their use
 #pragma unroll
@@ -521,24 +527,26 @@ struct Direct : Tile<WM_, WN_, TM_, TN_> {
         Base::clear(acc);
         const int64_t depth = x.depth;
         if (depth <= 0) return;
-        char* S = reinterpret_cast<char*>(lds);
+        const int set = WK > 1 ? __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) / (WM * WN)) : 0;
+        char* S = reinterpret_cast<char*>(lds) + set * kSet;
         X X_;
         Y Y_;
         X_.begin(x);
         Y_.begin(y);
+        const int64_t from = set * BK;
 #pragma unroll
         for (int t = 0; t < STAGES - 1; ++t) {
-            X_.load(x, t * BK, S + t * kStage);
-            Y_.load(y, t * BK, S + t * kStage + X::kSize);
+            X_.load(x, from + t * WK * BK, S + t * kStage);
+            Y_.load(y, from + t * WK * BK, S + t * kStage + X::kSize);
         }
         meet<kAhead>();
         Operands f[2];
         read(f[0], S, 0);
         int now = 0, next = STAGES - 1;                                       // stages of this step and of the one loaded
-        for (int64_t k0 = 0; k0 < depth; k0 += BK) {
+        for (int64_t k0 = 0; k0 < depth; k0 += WK * BK) {
             // into the stage of the step before, which nobody reads any more
-            X_.load(x, k0 + (STAGES - 1) * BK, S + next * kStage);
-            Y_.load(y, k0 + (STAGES - 1) * BK, S + next * kStage + X::kSize);
+            X_.load(x, from + k0 + (STAGES - 1) * WK * BK, S + next * kStage);
+            Y_.load(y, from + k0 + (STAGES - 1) * WK * BK, S + next * kStage + X::kSize);
 #pragma unroll
             for (int s = 0; s + 1 < SUBS; ++s) {
                 read(f[(s + 1) & 1], S + now * kStage, s + 1);
@@ -551,6 +559,26 @@ struct Direct : Tile<WM_, WN_, TM_, TN_> {
             add(acc, f[(SUBS - 1) & 1]);
         }
         meet<0>();                                                            // the LDS is free
+        if constexpr (WK > 1) {
+            float4* sums = reinterpret_cast<float4*>(lds + kSlabs) + threadIdx.x % (64 * WM * WN);
+            constexpr int EACH = 64 * WM * WN;                                // (of a set's lanes, a quad of results next to the other lanes')
+            if (set > 0)
+#pragma unroll
+                for (int q = 0; q < TM * TN * 4; ++q) {
+                    const floatx16& v = acc[q / 4 / TN][q / 4 % TN];
+                    sums[((set - 1) * TM * TN * 4 + q) * EACH] = make_float4(v[q % 4 * 4], v[q % 4 * 4 + 1], v[q % 4 * 4 + 2], v[q % 4 * 4 + 3]);
+                }
+            meet<0>();
+            if (set == 0)
+#pragma unroll
+                for (int t = 0; t < WK - 1; ++t)
+#pragma unroll
+                    for (int q = 0; q < TM * TN * 4; ++q) {
+                        const float4 u = sums[(t * TM * TN * 4 + q) * EACH];
+                        floatx16& v = acc[q / 4 / TN][q / 4 % TN];
+                        v[q % 4 * 4] += u.x; v[q % 4 * 4 + 1] += u.y; v[q % 4 * 4 + 2] += u.z; v[q % 4 * 4 + 3] += u.w;
+                    }
+        }
     }
 };
 
