@@ -156,7 +156,7 @@ struct Sizes {
 };
 template <class T, Lie X, Lie Y, Mode M>
 struct Sizes<T, X, Y, M, true> {
-    using Large = Direct<T, X, Y, 2, 4, 4, 2, 2>;              // 256 x 256
+    using Large = Direct<T, X, Y, 2, 2, 2, 4, 3, 1, 32>;       // 128 x 256
     using Middle = Direct<T, X, Y, 2, 2, 2, 2, 2>;             // 128 x 128
     using Small = Direct<T, X, Y, 2, 2, 1, 1, 4>;              // 64 x 64
     using Few = Direct<T, X, Y, 1, 2, 1, 1, 6>;                // 32 x 64
@@ -165,7 +165,7 @@ template <Size SIZE, class T, Lie X, Lie Y, Mode M>
 using Sized = std::conditional_t<SIZE == kLarge, typename Sizes<T, X, Y, M>::Large, std::conditional_t<SIZE == kMiddle, typename Sizes<T, X, Y, M>::Middle,
               std::conditional_t<SIZE == kSmall, typename Sizes<T, X, Y, M>::Small, typename Sizes<T, X, Y, M>::Few>>>;
 constexpr int kSizeCols[] = {256, 128, 64, 64};
-int size_rows(Size s, bool straight) { return s == kLarge ? straight ? 256 : 128 : s == kMiddle ? 128 : s == kSmall ? 64 : 32; }
+int size_rows(Size s, bool straight) { return s == kLarge ? 128 : s == kMiddle ? 128 : s == kSmall ? 64 : 32; }
 constexpr int64_t kCus = 256;
 
 int64_t over(int64_t a, int64_t b) { return (a + b - 1) / b; }

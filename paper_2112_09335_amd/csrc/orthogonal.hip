@@ -154,7 +154,7 @@ __device__ __forceinline__ void place(int tile_rows, int tile_cols, int64_t& b, 
 }
 
 // out = alpha X^T X or X X^T (LIE: kAlong forms X X^T), or with `from` = X symmetric: alpha X X + beta X + gamma 1.  The result is symmetric:
-// tiles below the diagonal are left out, and of the others every entry on or above it is stored to both its places.
+// tiles below the diagonal are left out, and those above it are stored to both their places.
 template <class P, Lie LIE>
 __global__ __launch_bounds__(P::THREADS, P::THREADS == 256 ? 2 : 1) void orthogonal_square_kernel(Stack x, int r, int64_t depth, Stack out, float alpha, float beta, float gamma,
                                                                           int with_linear, int tile_rows, int tile_cols) {
@@ -162,18 +162,18 @@ __global__ __launch_bounds__(P::THREADS, P::THREADS == 256 ? 2 : 1) void orthogo
     int64_t b;
     int ti, tj;
     place(tile_rows, tile_cols, b, ti, tj);
+    static_assert(P::BM == P::BN, "");
     const int i0 = ti * P::BM, c0 = tj * P::BN;
-    if (i0 >= c0 + P::BN) return;
+    if (ti > tj) return;
     floatx16 acc[P::TM][P::TN];
     if (LIE == kAlong) P::run(acc, x.view(b, i0, 0, r - i0, depth), x.view(b, c0, 0, r - c0, depth), S);
     else P::run(acc, x.view(b, 0, i0, x.width - i0, depth), x.view(b, 0, c0, x.width - c0, depth), S);
     _Float16* to = out.matrix(b);
     const _Float16* lin = x.matrix(b);
-    const bool crossing = c0 < i0 + P::BM;                 // the tile holds entries below the diagonal
     auto own = [&](int row, int col, float4 v) {
         const int i = i0 + row, j = c0 + col;
-        float w[4] = {alpha * v.x, alpha * v.y, alpha * v.z, alpha * v.w};
         if (i >= r || j >= out.width) return v;
+        float w[4] = {alpha * v.x, alpha * v.y, alpha * v.z, alpha * v.w};
         if (with_linear) {
             const f16x4 h = *reinterpret_cast<const f16x4*>(lin + x.at(i, j)), l = *reinterpret_cast<const f16x4*>(lin + x.at(i, j) + 8);
             const float s[4] = {(float)h.x + (float)l.x, (float)h.y + (float)l.y, (float)h.z + (float)l.z, (float)h.w + (float)l.w};
@@ -181,29 +181,13 @@ __global__ __launch_bounds__(P::THREADS, P::THREADS == 256 ? 2 : 1) void orthogo
             for (int e = 0; e < 4; ++e) w[e] = w[e] + beta * s[e] + (j + e == i ? gamma : 0.f);
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = j + e < r ? w[e] : 0.f;
+        for (int e = 0; e < 4; ++e) w[e] = j + e < r ? w[e] : 0.f;             // (columns r .. width hold zeros)
         const float4 q = make_float4(w[0], w[1], w[2], w[3]);
-        _Float16* at = to + out.at(i, j);
-        if (!crossing || j >= i) put_pair(at, q);
-        else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (j + e >= i) split_pair(w[e], at[e], at[e + 8]);
-        }
+        put_pair(to + out.at(i, j), q);
         return q;
     };
-    // ( columns r .. width hold zeros, which the own side of the last tile column leaves)
-    auto mirror = [&](int col, int row, float4 v) {
-        const int i = i0 + row, j = c0 + col;
-        if (j >= r || i >= r) return;
-        const float w[4] = {v.x, v.y, v.z, v.w};
-        _Float16* at = to + out.at(j, i);
-        if (i + 3 < j) put_pair(at, v);
-        else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (i + e < j) split_pair(w[e], at[e], at[e + 8]);
-        }
+    auto mirror = [&](int col, int row, float4 v) {                          // (above the diagonal every row is one of the r)
+        if (ti < tj && c0 + col < r) put_pair(to + out.at(c0 + col, i0 + row), v);
     };
     P::template drain<true>(acc, S, own, mirror);
 }
@@ -255,7 +239,7 @@ __global__ __launch_bounds__(P::THREADS, P::THREADS == 256 ? 2 : 1) void orthogo
 constexpr int kMostSteps = 64;
 struct Schedule { float s[kMostSteps], p2[kMostSteps], p1[kMostSteps], p0[kMostSteps], x[kMostSteps]; };      // factors of S, S^2, S, 1 and of X' a step
 constexpr int kBlockX = 65536, kBlockS = 65536;          // bytes of LDS
-constexpr int kMostSlabs = 16;
+constexpr int kMostSlabs = 16, kFewParts = 4;            // of one matrix; of which a workgroup adds up the parts of S itself
 
 // A wavefront's operands from rows of PIECES pieces of 16 bytes in LDS (a chunk's eight high parts, its eight low ones); the pieces of a row are
 // permuted by its number so that both the sixteen rows that are read along it at once and the four that are read across hit different
@@ -303,11 +287,19 @@ __device__ __forceinline__ floatx16 multiply_pairs(const uintx4 (&y)[2], const u
     return multiply<Pair>(y[0], x[0], c);
 }
 
+// f for the steps that begin below `most`, `each` apart (what lies behind is zeros); two at a time: a launch fetches this code anew.
+template <class F>
+__device__ __forceinline__ void over_steps(int most, int each, F f) {
+#pragma unroll 2
+    for (int s = 0; s * each < most; ++s) f(s);
+}
+
 // `one`: the whole polynomial (one slab); else step `step` of it, 0: only X and the first S.
 template <class T, int RT>
 __global__ __launch_bounds__(1024) void orthogonal_block_kernel(Source<T> src, const double* __restrict__ norms, int n_norms, int K, int C, float eps,
                                                                 float scale, int slabs, int one, int step, int steps, Schedule sch,
-                                                                char* __restrict__ images, float* __restrict__ parts_in, float* __restrict__ parts_out,
+                                                                char* __restrict__ images, const float* __restrict__ parts_in, int n_parts,
+                                                                float* __restrict__ parts_out,
                                                                 T* __restrict__ out, float* __restrict__ W, float keep, float rate) {
     constexpr int R = 32 * RT, WIDTH = kBlockX / 4 / R, CT = WIDTH / 32;         // rows, columns of the slab, tiles of 32 columns
     constexpr int GROUPS = 16 / (RT * RT);                                   // wavefronts that share a tile of S
@@ -338,7 +330,7 @@ __global__ __launch_bounds__(1024) void orthogonal_block_kernel(Source<T> src, c
         };
         if (tall) {
             // neighbouring threads take neighbouring elements in memory
-#pragma unroll 4
+#pragma unroll 2
             for (int f = tid; f < R * WIDTH; f += 1024) {
                 const int i = f % R, j = f / R;
                 _Float16* at = reinterpret_cast<_Float16*>(X + XRows::at(i, j));
@@ -346,7 +338,7 @@ __global__ __launch_bounds__(1024) void orthogonal_block_kernel(Source<T> src, c
                 split_pair(element(i, j), *at, *low);
             }
         } else {
-#pragma unroll 4
+#pragma unroll 1
             for (int f = tid; f < R * WIDTH / 4; f += 1024) {
                 const int i = f / (WIDTH / 4), j = f % (WIDTH / 4) * 4;
                 XRows::put(X, i, j, make_float4(element(i, j), element(i, j + 1), element(i, j + 2), element(i, j + 3)));
@@ -360,6 +352,7 @@ __global__ __launch_bounds__(1024) void orthogonal_block_kernel(Source<T> src, c
 
     const int tile = wave % (RT * RT), group = wave / (RT * RT), ti = tile / RT, tj = tile % RT;       // of S
     const int xi = wave / CT, xj = wave % CT;                                                 // of X
+    const bool holds = 32 * ti < r && 32 * tj < r;                             // (all else is zeros)
     floatx16 acc;
     // (parts in the accumulators' order: 16 numbers of a lane, lanes of a tile, tiles)
     auto load_sum = [&](const float* from) {
@@ -379,12 +372,11 @@ __global__ __launch_bounds__(1024) void orthogonal_block_kernel(Source<T> src, c
         __syncthreads();
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-#pragma unroll
-        for (int t = 0; t < WIDTH / 16 / GROUPS; ++t) {
-            const int s = group * (WIDTH / 16 / GROUPS) + t;
+        over_steps(holds ? ws - 16 * group : 0, 16 * GROUPS, [&](int t) {
+            const int s = t * GROUPS + group;
             const uintx4 x[2] = {XRows::along(X, ti, s, 0), XRows::along(X, ti, s, 1)}, y[2] = {XRows::along(X, tj, s, 0), XRows::along(X, tj, s, 1)};
             acc = multiply_pairs(y, x, acc);
-        }
+        });
     };
     auto join_groups = [&] {                                                   // to group 0
         if constexpr (GROUPS > 1) {
@@ -408,7 +400,7 @@ __global__ __launch_bounds__(1024) void orthogonal_block_kernel(Source<T> src, c
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[e] = 0.f;
 #pragma unroll 2
-            for (int t = group; t < slabs; t += GROUPS) acc += load_sum(parts_in + (b * slabs + t) * R * R);
+            for (int t = group; t < n_parts; t += GROUPS) acc += load_sum(parts_in + (b * n_parts + t) * R * R);
             __syncthreads();                                                 // (X is there)
         }
         join_groups();
@@ -422,11 +414,10 @@ __global__ __launch_bounds__(1024) void orthogonal_block_kernel(Source<T> src, c
         if (group == 0) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) square[e] = 0.f;
-#pragma unroll
-            for (int s = 0; s < R / 16; ++s) {
+            over_steps(holds ? r : 0, 16, [&](int s) {
                 const uintx4 x[2] = {SRows::along(S, ti, s, 0), SRows::along(S, ti, s, 1)}, y[2] = {SRows::along(S, tj, s, 0), SRows::along(S, tj, s, 1)};
                 square = multiply_pairs(y, x, square);
-            }
+            });
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int col = 32 * tj + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
@@ -438,15 +429,14 @@ __global__ __launch_bounds__(1024) void orthogonal_block_kernel(Source<T> src, c
         __syncthreads();
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-#pragma unroll
-        for (int s = 0; s < R / 16; ++s) {
+        over_steps(32 * xi < r && 32 * xj < ws ? r : 0, 16, [&](int s) {
             const uintx4 x[2] = {SRows::along(S, xi, s, 0), SRows::along(S, xi, s, 1)}, y[2] = {XRows::across(X, xj, s, 0), XRows::across(X, xj, s, 1)};
             acc = multiply_pairs(y, x, acc);
-        }
+        });
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[e] *= sch.x[k];
         __syncthreads();                                                     // (nobody reads the old X any more)
-        if (k + 1 < steps) XRows::put_tile(X, xi, xj, acc);
+        if (k + 1 < steps && 32 * xj < ws) XRows::put_tile(X, xi, xj, acc);
     }
     if (!one && step < steps) {
         if (step > 0) leave_part();
@@ -471,6 +461,20 @@ __global__ __launch_bounds__(1024) void orthogonal_block_kernel(Source<T> src, c
     if (tall) Out::template drain<true>(last, reinterpret_cast<unsigned short*>(lds), [](int, int, float4 v) { return v; },
                                         [&](int col, int row, float4 v) { if (col < ws) store(w0 + col, row, v); });
     else Out::drain(last, reinterpret_cast<unsigned short*>(lds), [&](int row, int col, float4 v) { store(row, w0 + col, v); });
+}
+
+// The slabs' parts of S, added up: with many slabs, every workgroup of the next step would read all of them.
+__global__ __launch_bounds__(256) void orthogonal_parts_kernel(const float* __restrict__ parts, int slabs, int size, float* __restrict__ sums) {
+    const int e = (blockIdx.x * 256 + threadIdx.x) * 4;
+    const float* from = parts + (int64_t)blockIdx.y * slabs * size + e;
+    float4 v[kMostSlabs];
+#pragma unroll
+    for (int t = 0; t < kMostSlabs; ++t) v[t] = *reinterpret_cast<const float4*>(from + (int64_t)(t < slabs ? t : 0) * size);
+    float4 s = v[0];
+#pragma unroll
+    for (int t = 1; t < kMostSlabs; ++t)
+        if (t < slabs) { s.x += v[t].x; s.y += v[t].y; s.z += v[t].z; s.w += v[t].w; }
+    *reinterpret_cast<float4*>(sums + (int64_t)blockIdx.y * size + e) = s;
 }
 
 template <Lie X, Lie Y> using Large = Direct<Pair, X, Y, 2, 4, 4, 2, 2>;         // 256 x 256
@@ -547,7 +551,7 @@ Layout layout(int64_t batch, int K, int C) {
     Layout l{0, 0, 0, 8 * kNormBlocks * batch + 5 * 256};
     if (bl.rt) {
         l.parts = batch * bl.slabs * (32 * bl.rt) * (32 * bl.rt);
-        if (bl.slabs > 1) l.bytes += batch * bl.slabs * kBlockX + 2 * 4 * l.parts;
+        if (bl.slabs > 1) l.bytes += batch * bl.slabs * kBlockX + 3 * 4 * l.parts;
     } else {
         l.x = batch * K * row_pairs(C);
         l.s = batch * r * row_pairs(r);
@@ -585,10 +589,16 @@ void launch_blocks(hipStream_t s, const Orthogonal& a, const Source<T>& src, int
         sch.x[k] = std::ldexp(1.f, (k + 1 == a.steps ? 0 : e.next) - e.p - e.x);
     }
     const float scale = std::ldexp(1.f, scale_for(1.0));
-    for (int step = slabs > 1 ? 0 : a.steps; step <= a.steps; ++step)
+    const int size = 1024 * RT * RT;
+    const bool summed = slabs > kFewParts;
+    float* sums = parts + 2 * part_floats;
+    for (int step = slabs > 1 ? 0 : a.steps; step <= a.steps; ++step) {
+        const float* in = parts + (step + 1) % 2 * part_floats;
+        if (summed && step > 0) orthogonal_parts_kernel<<<dim3(size / 1024, a.batch), dim3(256), 0, s>>>(in, slabs, size, sums);
         orthogonal_block_kernel<T, RT><<<dim3((unsigned)(a.batch * slabs)), dim3(1024), 0, s>>>(
-            src, norms, n_norms, a.K, a.C, a.eps, scale, slabs, slabs == 1, step, a.steps, sch, images, parts + (step + 1) % 2 * part_floats,
+            src, norms, n_norms, a.K, a.C, a.eps, scale, slabs, slabs == 1, step, a.steps, sch, images, summed ? sums : in, summed ? 1 : slabs,
             parts + step % 2 * part_floats, (T*)a.out, a.W, a.keep, a.rate);
+    }
 }
 }  // namespace
 
@@ -615,7 +625,7 @@ void launch_orthogonalise(hipStream_t s, int type, const Orthogonal& a) {
         if (bl.slabs != 1) orthogonal_norm_kernel<T><<<dim3(nb, a.batch), dim3(256), 0, s>>>(src, count, norms);
         if (!bl.rt) return;
         char* images = take(bl.slabs > 1 ? (int64_t)a.batch * bl.slabs * kBlockX : 0);
-        float* parts = (float*)take(bl.slabs > 1 ? 2 * 4 * l.parts : 0);
+        float* parts = (float*)take(bl.slabs > 1 ? 3 * 4 * l.parts : 0);
         if (bl.rt == 2) launch_blocks<T, 2>(s, a, src, bl.slabs, norms, nb, images, parts, l.parts);
         else launch_blocks<T, 4>(s, a, src, bl.slabs, norms, nb, images, parts, l.parts);
     });

@@ -405,7 +405,7 @@ struct Product : Tile<WM_, WN_, TM_, TN_> {
 };
 
 // Tiles whose operands go from memory straight to LDS, STAGES - 1 steps ahead: bf16, fp16 and Pairs whose chunks are whole.  An LDS tile
-// is made of pieces of 16 bytes, of a chunk of 16-bit numbers or of a chunk's high or low parts, as they come in memory: rows of 128 bytes
+// is made of pieces of 16 bytes, of a chunk of 16-bit numbers or of a chunk's high or low parts, as they come in memory: rows of 128 or 64 bytes
 // (kAlong), or BK rows of the tile's width (kAcross); an instruction of a wavefront fills 64 pieces in a row, and which piece of memory a
 // lane brings is chosen so that the 32 lanes that read at a time find theirs in different banks.  One barrier per step; the first
 // operands of a step are read under the last matrix instructions of the one before.  32 x 2048 x 1024 x 1024 Pairs: 868 -> 997 TFLOP/s
@@ -419,10 +419,10 @@ struct DirectOperand {
     static constexpr int kPerRow = (LIE == kAlong ? BK : ROWS) * kBytes / 16;   // pieces of a row in memory
     static constexpr int kSize = ROWS * BK * kBytes;                          // bytes of a stage
     static constexpr int kEach = kSize / 1024 / WAVES;                        // instructions of a wavefront per stage
-    static_assert(kEach * 1024 * WAVES == kSize && (LIE == kAcross || kPerRow == 8), "");
+    static_assert(kEach * 1024 * WAVES == kSize && (LIE == kAcross || kPerRow == 8 || kPerRow == 4), "");
     unsigned from[kEach];
     __device__ __forceinline__ static int swizzle(int row) {
-        if constexpr (LIE == kAlong) return row >> 1 & 7;
+        if constexpr (LIE == kAlong) return kPerRow == 8 ? row >> 1 & 7 : row >> 2 & 3;
         else if constexpr (kParts_ == 2) return kPerRow >= 16 ? (row & 1) | (row & 2) << 2 : 0;
         else return kPerRow >= 16 ? (row & 3) << 2 : kPerRow == 8 ? (row & 2) << 1 : 0;
     }
@@ -447,7 +447,7 @@ struct DirectOperand {
         const char* base = reinterpret_cast<const char*>(x.p) + (LIE == kAlong ? k0 * kBytes : k0 * x.ld * (int64_t)sizeof(E));
         S += __builtin_amdgcn_readfirstlane(wave()) * 1024;
         const int64_t left = x.depth - k0;
-        if (left >= BK) {                                                     // (uniform)
+        if (kEach > 2 && left >= BK) {                                         // (uniform; small tiles: less code rather than fewer instructions)
 #pragma unroll
             for (int u = 0; u < kEach; ++u) __builtin_amdgcn_global_load_lds((Global)(base + from[u]), (Local)(S + u * WAVES * 1024), 16, 0, 0);
         } else {                                                              // what lies past the end of the contraction is zero
@@ -464,7 +464,7 @@ struct DirectOperand {
         const int lane = threadIdx.x & 63;
         if constexpr (LIE == kAlong) {
             const int row = 32 * b + (lane & 31), piece = (2 * s + (lane >> 5)) * kParts_ + p;
-            return *reinterpret_cast<const uintx4*>(S + row * 128 + ((piece ^ swizzle(row)) << 4));
+            return *reinterpret_cast<const uintx4*>(S + (row * kPerRow + (piece ^ swizzle(row))) * 16);
         } else {
             const int k = 16 * s + 8 * (lane >> 5) + ((lane & 15) >> 2), col = 32 * b + (lane & 16) + 4 * (lane & 3);
             const char* from = S + (k * kPerRow + (((col >> 3) * kParts_ + p) ^ swizzle(k))) * 16 + (col & 4) * 2;
@@ -479,11 +479,11 @@ struct DirectOperand {
     }
 };
 
-template <class T, Lie XL, Lie YL, int WM_, int WN_, int TM_, int TN_, int STAGES_, int WK_ = 1>
+template <class T, Lie XL, Lie YL, int WM_, int WN_, int TM_, int TN_, int STAGES_, int WK_ = 1, int BK_ = 64 / kParts<T>>
 struct Direct : Tile<WM_, WN_, TM_, TN_, WK_> {
     using Base = Tile<WM_, WN_, TM_, TN_, WK_>;
     using Base::WM; using Base::WN; using Base::TM; using Base::TN; using Base::WK; using Base::BM; using Base::BN; using Base::THREADS; using Base::kSlabs;
-    static constexpr int P = kParts<T>, BK = 64 / P, SUBS = BK / 16, STAGES = STAGES_;
+    static constexpr int P = kParts<T>, BK = BK_, SUBS = BK / 16, STAGES = STAGES_;
     using X = DirectOperand<T, XL, BM, BK, WM * WN>;
     using Y = DirectOperand<T, YL, BN, BK, WM * WN>;
     static constexpr int kStage = X::kSize + Y::kSize;
@@ -534,7 +534,7 @@ struct Direct : Tile<WM_, WN_, TM_, TN_, WK_> {
         X_.begin(x);
         Y_.begin(y);
         const int64_t from = set * BK;
-#pragma unroll
+#pragma unroll 1
         for (int t = 0; t < STAGES - 1; ++t) {
             X_.load(x, from + t * WK * BK, S + t * kStage);
             Y_.load(y, from + t * WK * BK, S + t * kStage + X::kSize);
