@@ -143,52 +143,65 @@ void with_type(int type, F f) {
 }
 
 // Tiles: wavefronts, 32 x 32 accumulators of one; then, through registers, contraction per step, steps ahead, LDS buffers, or, straight to
-// LDS, stages.  Large ones read each operand from LDS once for 128 x 256 results, two workgroups a compute unit, or for 256 x 256,
-// one; the small ones are for products that would not fill the chip with them.
+// LDS, stages, sets of wavefronts and contraction per step.
+//   kLarge  operands are read from LDS once for 128 x 256 results (two workgroups a compute unit) or 256 x 256.  16-bit transform, K = 512,
+//           500000 rows: 128 x 256 391 us, 256 x 256 407, 128 x 128 431 (a library product of one matrix: 389); fp32, through registers,
+//           is faster in 128 x 128 at every size tried (200000 x 256 x 256 165 us for 171) and has no larger ones.  16-bit wgrad:
+//           256 x 256 202 us, 128 x 256 214 (16384 x 2048 x 1024, 64 groups).
+//   kMiddle 128 x 128;  kSmall 64 x 64, where larger ones would not give every compute unit one
+//   kFew    32 x 64, for groups of a few rows: reading the weights is all there is to it, from many places and far ahead.
 template <class T> constexpr int kStep = 128 / sizeof(T);
 enum Size { kLarge, kMiddle, kSmall, kFew };
 template <class T, Lie X, Lie Y, Mode M, bool STRAIGHT = sizeof(T) == 2 && M == kWhole>
 struct Sizes {
-    using Large = Product<T, X, Y, M, 2, 2, 2, 4, X == kAlong ? kStep<T> : kStep<T> / 2, 1, 1>;          // 128 x 256
-    using Middle = Product<T, X, Y, M, 2, 2, 2, 2, kStep<T>, 1, 1>;                                   // 128 x 128
-    using Small = Product<T, X, Y, M, 2, 2, 1, 1, kStep<T>, 2, 2>;                                    // 64 x 64
-    using Few = Product<T, X, Y, M, 1, 2, 1, 1, kStep<T>, 4, 2>;                                      // 32 x 64
+    using Large = Product<T, X, Y, M, 2, 2, 2, 4, kStep<T> / 2, 1, 1>;
+    using Middle = Product<T, X, Y, M, 2, 2, 2, 2, kStep<T>, 1, 1>;
+    using Small = Product<T, X, Y, M, 2, 2, 1, 1, kStep<T>, 2, 2>;
+    using Few = Product<T, X, Y, M, 1, 2, 1, 1, kStep<T>, 4, 2>;
 };
 template <class T, Lie X, Lie Y, Mode M>
 struct Sizes<T, X, Y, M, true> {
-    using Large = Direct<T, X, Y, 2, 2, 2, 4, 3, 1, 32>;       // 128 x 256
-    using Middle = Direct<T, X, Y, 2, 2, 2, 2, 2>;             // 128 x 128
-    using Small = Direct<T, X, Y, 2, 2, 1, 1, 4>;              // 64 x 64
-    using Few = Direct<T, X, Y, 1, 2, 1, 1, 6>;                // 32 x 64
+    using Large = std::conditional_t<X == kAlong, Direct<T, X, Y, 2, 2, 2, 4, 3, 1, 32>, Direct<T, X, Y, 2, 4, 4, 2, 2>>;
+    using Middle = Direct<T, X, Y, 2, 2, 2, 2, 2>;
+    using Small = Direct<T, X, Y, 2, 2, 1, 1, 4>;
+    using Few = Direct<T, X, Y, 1, 2, 1, 1, 6, 2>;
 };
 template <Size SIZE, class T, Lie X, Lie Y, Mode M>
 using Sized = std::conditional_t<SIZE == kLarge, typename Sizes<T, X, Y, M>::Large, std::conditional_t<SIZE == kMiddle, typename Sizes<T, X, Y, M>::Middle,
               std::conditional_t<SIZE == kSmall, typename Sizes<T, X, Y, M>::Small, typename Sizes<T, X, Y, M>::Few>>>;
-constexpr int kSizeCols[] = {256, 128, 64, 64};
-int size_rows(Size s, bool straight) { return s == kLarge ? 128 : s == kMiddle ? 128 : s == kSmall ? 64 : 32; }
+constexpr int kSizeCols[] = {256, 128, 64, 64}, kNnRows[] = {128, 128, 64, 32};
+int tn_rows(Size s, bool straight) { return s == kLarge ? straight ? 256 : 128 : kNnRows[s]; }
 constexpr int64_t kCus = 256;
 
 int64_t over(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// The largest tiles that give every compute unit a workgroup.
 Size nn_size(int64_t n, int C, int groups, bool straight) {
     const int64_t hit = std::min<int64_t>(n, groups), rows = over(n, hit);            // rows of a group that has any, if they share alike
     for (Size s : {kLarge, kMiddle, kSmall}) {
-        const int r = size_rows(s, straight);
-        const bool fits = C > kSizeCols[s] / 2 && rows > r / 2;
-        if (fits && (n / r + hit / 2) * over(C, kSizeCols[s]) >= kCus) return s;
+        if (s == kLarge && !straight) continue;
+        const bool fits = C > kSizeCols[s] / 2 && rows > kNnRows[s] / 2;
+        if (fits && (n / kNnRows[s] + hit / 2) * over(C, kSizeCols[s]) >= kCus) return s;
     }
     return rows > 32 ? kSmall : kFew;
 }
 
 struct TnPlan { Size size; int64_t most, parts; };
 TnPlan tn_plan(int64_t n, int K, int C, int groups, bool straight) {
-    const Size s = K > size_rows(kLarge, straight) / 2 && C > 128 ? kLarge : K > 64 && C > 64 ? kMiddle : kSmall;
-    const int64_t tiles = over(K, size_rows(s, straight)) * over(C, kSizeCols[s]);
-    TnPlan p{s, n > 0 ? n : 1, 0};
-    // too few tiles for two workgroups a compute unit: the rows are shared out too, 256 of them at least
-    if (tiles * groups < 2 * kCus * 2) p.most = std::max<int64_t>(256, over(over(n * tiles, 2 * kCus), 64) * 64);
-    p.parts = p.most < n ? 2 * (n / p.most + 1) : 0;
-    return p;
+    for (Size s : {kLarge, kMiddle, kSmall}) {
+        const int rows = tn_rows(s, straight);
+        if (s != kSmall && (K <= rows / 2 || C <= kSizeCols[s] / 2)) continue;
+        const int64_t tiles = over(K, rows) * over(C, kSizeCols[s]);
+        TnPlan p{s, n > 0 ? n : 1, 0};
+        // too few tiles for two workgroups a compute unit: the rows are shared out too, 256 of them at least; large tiles only where 512 are
+        // left to each (20000 x 512 x 512 fp32 in 8 groups: 128 x 256 104 us, 128 x 128 88; 200000 x 256 x 256: 169 and 207)
+        const int64_t share = over(n * tiles, 2 * kCus);
+        if (s == kLarge && share < 512) continue;
+        if (tiles * groups < 2 * kCus * 2) p.most = std::max<int64_t>(256, over(share, 64) * 64);
+        p.parts = p.most < n ? 2 * (n / p.most + 1) : 0;
+        return p;
+    }
+    return {};
 }
 int64_t part_floats(int K, int C) { return over((int64_t)K * C, 4) * 4; }
 
@@ -203,8 +216,9 @@ void nn_launch(hipStream_t s, const GroupedNN& a, Size size, bool whole_out) {
         grouped_nn_kernel<P, T, YL><<<dim3((unsigned)blocks), dim3(P::THREADS), 0, s>>>(
             (const T*)a.A, a.n, a.lda, a.K, (const T*)a.B, a.C, a.groups, a.ptr, (T*)a.out, a.ldo, col_tiles, a.n / P::BM >= a.groups, whole_out);
     };
-    if (size == kLarge) go(std::integral_constant<Size, kLarge>());
-    else if (size == kMiddle) go(std::integral_constant<Size, kMiddle>());
+    if (size == kLarge) {
+        if constexpr (sizeof(T) == 2 && MODE == kWhole) go(std::integral_constant<Size, kLarge>());
+    } else if (size == kMiddle) go(std::integral_constant<Size, kMiddle>());
     else if (size == kSmall) go(std::integral_constant<Size, kSmall>());
     else go(std::integral_constant<Size, kFew>());
 }
@@ -240,7 +254,7 @@ int64_t grouped_nn_blocks(int64_t n, int C, int groups) {
     for (bool straight : {false, true}) {
         if (n == 0) continue;
         const Size s = nn_size(n, C, groups, straight);
-        most = std::max(most, (n / size_rows(s, straight) + groups) * over(C, kSizeCols[s]));
+        most = std::max(most, (n / kNnRows[s] + groups) * over(C, kSizeCols[s]));
     }
     return most;
 }
@@ -248,7 +262,7 @@ int64_t grouped_tn_blocks(int64_t n, int K, int C, int groups) {
     int64_t most = 0;
     for (bool straight : {false, true}) {
         const TnPlan p = tn_plan(n, K, C, groups, straight);
-        most = std::max(most, (n / p.most + groups) * over(K, size_rows(p.size, straight)) * over(C, kSizeCols[p.size]));
+        most = std::max(most, (n / p.most + groups) * over(K, tn_rows(p.size, straight)) * over(C, kSizeCols[p.size]));
     }
     return most;
 }

@@ -497,7 +497,7 @@ constexpr int64_t kCus = 256;
 Size size_of(int64_t batch, int64_t rows, int64_t cols, bool half) {
     for (Size s : {kLarge, kMiddle})
         if (batch * over(rows, kSizeRows[s]) * over(cols, kSizeCols[s]) >= (half ? 2 : 1) * kCus) return s;
-    return batch * over(rows, 64) * over(cols, 64) > (half ? 2 : 1) * kCus ? kSmall : kLone;
+    return batch * over(rows, 64) * over(cols, 64) > kCus ? kSmall : kLone;
 }
 template <class F>
 void with_size(Size s, F f) {
