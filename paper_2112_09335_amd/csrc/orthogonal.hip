@@ -493,11 +493,15 @@ int64_t round8(int64_t n) { return (n + 7) / 8 * 8; }
 // channels (256 bytes each, 16 of them).
 int64_t row_pairs(int64_t n) { return n <= 64 ? round8(n) : (over(n, 64) | 1) * 64; }
 constexpr int64_t kCus = 256;
-// The largest tiles that give every compute unit one; half: of a symmetric result only that much is formed.
-Size size_of(int64_t batch, int64_t rows, int64_t cols, bool half) {
-    for (Size s : {kLarge, kMiddle})
-        if (batch * over(rows, kSizeRows[s]) * over(cols, kSizeCols[s]) >= (half ? 2 : 1) * kCus) return s;
-    return batch * over(rows, 64) * over(cols, 64) > kCus ? kSmall : kLone;
+// The largest tiles that give every compute unit one; of a symmetric result about half of them are formed, and large ones pay from
+// four a compute unit on (32 x 1024 x 1024 in 320 tiles of 256 x 256: 320 and 182 us, in 1152 of 128 x 128: 296 and 169).  Up to one small tile a
+// compute unit, sixteen wavefronts share its contraction, else eight (767 x 1000: 194 us a call for 216 with eight everywhere; 7 x 512 x 512: 193
+// for 260 with sixteen everywhere).
+Size size_of(int64_t batch, int64_t rows, int64_t cols, bool symmetric) {
+    auto tiles = [&](Size s) { return batch * over(rows, kSizeRows[s]) * over(cols, kSizeCols[s]); };
+    if (tiles(kLarge) >= (symmetric ? 8 : 1) * kCus) return kLarge;
+    if (tiles(kMiddle) >= (symmetric ? 2 : 1) * kCus) return kMiddle;
+    return tiles(kSmall) > kCus ? kSmall : kLone;
 }
 template <class F>
 void with_size(Size s, F f) {

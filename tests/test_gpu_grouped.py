@@ -90,6 +90,47 @@ def test_product_over_groups(solver, kind, transposed, sizes, K, width):
     close(out, *want_nn(A, B, ptr, transposed), K, kind)
 
 
+def on_gpu_nn(torch, A, B, ptr, transposed):
+    """want_nn with its products in 64 bits on the GPU: for sizes that fill it."""
+    out = torch.zeros((A.shape[0], B.shape[1 if transposed else 2]), dtype=torch.float64, device="cuda")
+    size = torch.zeros_like(out)
+    for g in range(ptr.shape[0] - 1):
+        lo, hi = int(ptr[g]), int(ptr[g + 1])
+        Bg = (B[g].T if transposed else B[g]).double().cuda().contiguous()
+        Ag = A[lo:hi].double().cuda()
+        out[lo:hi], size[lo:hi] = Ag @ Bg, Ag.abs() @ Bg.abs()
+    return out.cpu().numpy(), size.cpu().numpy()
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("sizes,K,width", [([9000, 0, 17001, 5, 14000], 136, 392), ([20000, 30, 20000], 520, 264), ([33000], 72, 512), ([11000, 9001], 200, 301),
+                                           ([1200] * 12, 1032, 640)], ids=lambda v: str(v).replace(" ", "")[:24])
+def test_product_over_groups_that_fills_the_chip(solver, kind, transposed, sizes, K, width):
+    import torch
+    A, B, ptr = draw(torch, K + width, sizes, K, width, kind, transposed)
+    out = solver.op_transform_grouped(A.cuda(), B.cuda(), ptr.cuda(), transposed=transposed)
+    close(out, *on_gpu_nn(torch, A, B, ptr, transposed), K, kind)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("sizes,K,width", [([30000, 0, 41000, 7], 264, 392), ([60000], 520, 520), ([40000, 20001], 301, 200), ([700] * 40, 1024, 1032)],
+                         ids=lambda v: str(v).replace(" ", "")[:24])
+def test_weight_gradient_over_groups_that_fills_the_chip(solver, kind, sizes, K, width):
+    import torch
+    A, _, ptr = draw(torch, K + width, sizes, K, 1, kind)
+    G, _, _ = draw(torch, K + width + 1, sizes, width, 1, kind, scale=2.0 ** -5)
+    want = torch.zeros((len(sizes), K, width), dtype=torch.float64, device="cuda")
+    size = torch.zeros_like(want)
+    for g in range(len(sizes)):
+        lo, hi = int(ptr[g]), int(ptr[g + 1])
+        a, b = A[lo:hi].double().T.contiguous().cuda(), G[lo:hi].double().cuda()
+        want[g], size[g] = a @ b, a.abs() @ b.abs()
+    out = solver.op_wgrad_grouped(A.cuda(), G.cuda(), ptr.cuda())
+    close(out, want.cpu().numpy(), size.cpu().numpy(), max(sizes), "f32")
+    assert torch.equal(out, solver.op_wgrad_grouped(A.cuda(), G.cuda(), ptr.cuda()))
+
+
 @pytest.mark.parametrize("kind,out_kind", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16"), ("f16", "f32"), ("f16", "f16")])
 @pytest.mark.parametrize("sizes,K,width", SHAPES + [([20000, 3, 9000], 64, 48), ([70000], 24, 5), ([4096, 4097], 256, 256), ([40000], 130, 130)],
                          ids=lambda v: str(v).replace(" ", "")[:24])

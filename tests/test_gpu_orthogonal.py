@@ -82,6 +82,17 @@ def test_orthogonalised_stack(solver, kind, batch, K, width):
         assert torch.equal(solver.op_orthogonalise(G[0].cuda()), out[0])
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("times,K,width", [(25, 520, 700), (70, 700, 520), (100, 300, 513), (30, 130, 129), (300, 64, 100), (100, 128, 300)])
+def test_stacks_that_fill_the_chip(solver, kind, times, K, width):
+    """Three matrices, each many times in the stack: the first of each against the polynomial, the others against the first."""
+    import torch
+    G = gradient(torch, K + width, 3, K, width, kind)
+    out = solver.op_orthogonalise(G.repeat(times, 1, 1).cuda()).view(times, 3, K, width)
+    assert all(torch.equal(out[0], out[i]) for i in range(1, times))
+    check(out[0].cpu(), G, kind)
+
+
 @pytest.mark.parametrize("coefficients,steps", [(MUON, 1), (MUON, 2), (MUON, 10), ((1.5, -0.5, 0.0), 12), ((15 / 8, -10 / 8, 3 / 8), 8), ((4.0, 0.0, 0.0), 4),
                                                 ((0.0, 1.0, 0.0), 1), ((-2.0, 0.5, 0.25), 3), ((0.5, 0.0, 0.0), 3)])
 @pytest.mark.parametrize("batch,K,width", [(2, 48, 80), (1, 260, 130), (1, 128, 512)])
