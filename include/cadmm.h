@@ -249,7 +249,7 @@ int  cadmm_op_wgrad_noalloc(cadmm_ctx* ctx, const float* A, const float* G, int6
  * No atomics: the same call gives the same bits.  n = 0 is allowed (A, G and transform_grouped's out may then be null).
  * wgrad_grouped needs device scratch of _scratch bytes, 256-byte aligned, that no other call uses until it is done; nothing in
  * it has to be cleared.  Neither call needs a graph, model or workspace.  Both run on the stream of the kernel-level calls and make the
- * context's device current for themselves.  At most 65536 columns and 2^20 groups.
+ * context's device current for themselves.  At most 65536 columns, 2^20 groups, and result tiles for 2^22 workgroups (CADMM_EUNSUPPORTED beyond).
  */
 #define CADMM_F32  0
 #define CADMM_BF16 1
@@ -269,12 +269,13 @@ int  cadmm_op_wgrad_grouped(cadmm_ctx* ctx, int32_t type, const void* A, int64_t
  *                   X <- a X + (b S + c S^2) X,  S = X X^T (K <= C; else the same of the transpose), coefficients = host {a, b, c}:
  *                   singular vectors stay, a singular value x becomes a x + b x^3 + c x^5.  out: device, as G.  A zero matrix gives
  *                   zeros (with eps = 0 too), one with an entry that is not finite NaNs throughout; the other matrices are not
- *                   concerned.  Entries of X are held to 2^-36 of one: of a G far below eps, little is left.  out may be G itself; it overlaps it in no other way.
+ *                   concerned.  Entries of X are held to 2^-36 of one: of a G far below eps, little is left.
+ *                   out may be G itself, and overlaps it in no other way.
  *   muon_step:      M <- momentum M + G;  D = G + momentum M with nesterov, else M;  W <- (1 - lr weight_decay) W - lr scale O with
  *                   O the orthogonalised D.  W, M: device batch x K x C, fp32, updated in place; G of `type`, not changed.  The three
  *                   do not overlap.
  * 1 <= steps <= 64; eps >= 0; coefficients under which a singular value in [0, 1] could grow past 1024 on the way are CADMM_EINVAL.  Products take
- * their operands with at least 22 bits and are summed in fp32, norms in fp64.  No atomics: the same call gives the
+ * their operands with 22 bits (pairs of fp16) and are summed in fp32, norms in fp64.  No atomics: the same call gives the
  * same bits.  scratch: device, _scratch bytes, 256-byte aligned, used by no other call until this one is done; nothing in it has to be
  * cleared.  Neither call needs a graph, model or workspace; streams and devices as for the products over groups.  At most 32768 rows or
  * columns and 65535 matrices (CADMM_EUNSUPPORTED).

@@ -1230,11 +1230,15 @@ int on_own_device(cadmm_ctx* c, const char* what, F body) {
     return rc;
 }
 
+bool overlap(const void* p, double p_bytes, const void* q, double q_bytes) {
+    const double a = (double)reinterpret_cast<uintptr_t>(p), b = (double)reinterpret_cast<uintptr_t>(q);
+    return p && q && a < b + q_bytes && b < a + p_bytes;
+}
 size_t type_bytes(int32_t type) { return type == CADMM_F32 ? 4 : 2; }
 bool known_type(int32_t type) { return type == CADMM_F32 || type == CADMM_BF16 || type == CADMM_F16; }
 bool misaligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
-constexpr int64_t kMostWidth = 1 << 16, kMostGroups = 1 << 20, kMostRows = (int64_t)1 << 40, kMostBlocks = 0x7fffffff;
+constexpr int64_t kMostWidth = 1 << 16, kMostGroups = 1 << 20, kMostRows = (int64_t)1 << 40, kMostBlocks = (1 << 22) - 1;   // (2^32 threads a launch, 1024 a workgroup)
 constexpr float kMostGrowth = 1024.f;            // singular values of the polynomial's iterates
 
 // What the products over groups ask of their sizes; "" or what is wrong.
@@ -1247,8 +1251,8 @@ const char* grouped_fault(int64_t n, int64_t lda, int32_t K, int64_t ldc, int32_
     return "";
 }
 
-// The largest singular value of the iterates after `steps` applications of x (a + b x^2 + c x^4) to values in [0, 1]; growth[k]: the
-// bound before step k.  A value that is not finite comes back as such.
+// The largest singular value that `steps` applications of x (a + b x^2 + c x^4) can make of values in [0, 1], or some value beyond all
+// bounds.
 double polynomial_growth(double a, double b, double c, int steps) {
     double s = 1.0, most = 1.0;
     for (int k = 0; k < steps; ++k) {
@@ -1984,6 +1988,10 @@ int orthogonalise(cadmm_ctx* c, const char* what, int32_t type, Orthogonal a, co
     const size_t bytes = type_bytes(type);
     if (misaligned(a.G, bytes) || misaligned(a.out, bytes) || misaligned(a.W, 4) || misaligned(a.M, 4))
         return fail(c, CADMM_EINVAL, "a pointer is not aligned to its elements");
+    const double entries = (double)a.batch * a.K * a.C, own = entries * bytes;
+    if (overlap(a.W, 4 * entries, a.M, 4 * entries) || overlap(a.W, 4 * entries, a.G, own) || overlap(a.M, 4 * entries, a.G, own) ||
+        (a.out != a.G && overlap(a.out, own, a.G, own)))
+        return fail(c, CADMM_EINVAL, "matrices overlap");
     if (misaligned(a.scratch, 256)) return fail(c, CADMM_EINVAL, "scratch must be 256-byte aligned");
     if (scratch_bytes < orthogonal_scratch(a.batch, a.K, a.C)) return fail(c, CADMM_ENOMEM, "scratch is smaller than cadmm_op_orthogonalise_scratch says");
     if (c->device < 0) return fail(c, CADMM_EUNSUPPORTED, "host-only context (device -1) has no device path");

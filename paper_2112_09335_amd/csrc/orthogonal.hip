@@ -535,7 +535,7 @@ double polynomial_bound(double a, double b, double c, double s) {
 const char* orthogonal_fault(int batch, int K, int C) {
     if (K > 32768 || C > 32768) return "matrices of more than 32768 rows or columns";
     if (batch > 65535) return "more than 65535 matrices";
-    if (over(K, 64) * over(C, 64) * batch > 0x7fffffff || over(std::min(K, C), 64) * over(std::min(K, C), 64) * batch > 0x7fffffff)
+    if (over(K, 64) * over(C, 64) * batch >= 1 << 22)                    // (2^32 threads a launch)
         return "more result tiles than one launch holds";
     return "";
 }

@@ -31,7 +31,7 @@ def ortho(s, type=0, G=BUF, batch=2, K=8, width=4, steps=5, coefficients=MUON, e
     return s.lib.cadmm_op_orthogonalise(s.h, type, G, batch, K, width, steps, c, eps, out, scratch, bytes)
 
 
-def muon(s, type=0, G=BUF, W=BUF, M=BUF, batch=2, K=8, width=4, lr=0.1, momentum=0.9, nesterov=1, decay=0.0, scale=1.0, steps=5,
+def muon(s, type=0, G=BUF, W=BUF + 0x10000, M=BUF + 0x20000, batch=2, K=8, width=4, lr=0.1, momentum=0.9, nesterov=1, decay=0.0, scale=1.0, steps=5,
          coefficients=MUON, eps=1e-7, scratch=BUF, bytes=1 << 40):
     c = None if coefficients is None else (C.c_float * 3)(*coefficients)
     return s.lib.cadmm_op_muon_step(s.h, type, G, W, M, batch, K, width, lr, momentum, nesterov, decay, scale, steps, c, eps, scratch, bytes)
@@ -52,12 +52,20 @@ def test_refusals_of_the_product_over_groups(host, wrong):
     assert transform(host, **wrong) == EINVAL
 
 
+def test_an_output_that_overlaps_its_input_in_part_is_refused(host):
+    size = 2 * 8 * 4 * 4
+    assert ortho(host, out=BUF) == EUNSUPPORTED and ortho(host, out=BUF + size) == EUNSUPPORTED and ortho(host, G=BUF + size) == EUNSUPPORTED
+    assert ortho(host, out=BUF + size - 4) == EINVAL and ortho(host, G=BUF + size - 4) == EINVAL
+
+
 def test_a_product_of_no_rows_is_done(host):
     assert transform(host, n=0, A=None, out=None) in (OK, EUNSUPPORTED)
 
 
 def test_a_product_of_too_many_tiles_is_not_supported(host):
-    assert transform(host, n=1 << 40, width=60000, ldo=60000) in (EUNSUPPORTED, EINVAL)
+    assert transform(host, n=1 << 40, lda=8, width=60, ldo=60) == EUNSUPPORTED
+    assert wgrad(host, K=60000, lda=60000, width=60000, ldg=60000, groups=1 << 20) == EUNSUPPORTED
+    assert ortho(host, K=32768, width=32768, batch=1000) == EUNSUPPORTED
 
 
 @pytest.mark.parametrize("wrong,code", [
@@ -103,7 +111,9 @@ def test_coefficients_that_keep_singular_values_in_bounds_are_taken(host, coeffi
     assert ortho(host, coefficients=coefficients, steps=steps) == EUNSUPPORTED                   # (for want of a device)
 
 
-@pytest.mark.parametrize("wrong", [dict(W=None), dict(M=None), dict(W=BUF + 2), dict(M=BUF + 1), dict(lr=float("nan")), dict(momentum=float("inf")),
+@pytest.mark.parametrize("wrong", [dict(W=None), dict(M=None), dict(W=BUF + 0x10002), dict(M=BUF + 0x20001),
+                                   dict(W=BUF + 0x20000), dict(G=BUF + 0x10000), dict(M=BUF + 252), dict(G=BUF + 0x20004),
+                                   dict(lr=float("nan")), dict(momentum=float("inf")),
                                    dict(decay=float("nan")), dict(scale=float("inf"))])
 def test_refusals_of_the_optimiser_step(host, wrong):
     assert muon(host, **wrong) == EINVAL
@@ -125,7 +135,7 @@ CALLS = [
     lambda t: lib.cadmm_op_wgrad_grouped(h, t, buf, 100000, 64, 64, buf, 48, 48, 4, buf, 0, buf, buf, 1 << 40),
     lambda t: lib.cadmm_op_orthogonalise(h, t, buf, 3, 64, 48, 5, co, 1e-7, buf, buf, 1 << 40),
     lambda t: lib.cadmm_op_orthogonalise(h, t, buf, 3, 640, 700, 2, co, 1e-7, buf, buf, 1 << 40),
-    lambda t: lib.cadmm_op_muon_step(h, t, buf, buf, buf, 3, 64, 48, .1, .9, 1, 0., 1., 5, co, 1e-7, buf, 1 << 40),
+    lambda t: lib.cadmm_op_muon_step(h, t, buf, 2 * buf, 3 * buf, 3, 64, 48, .1, .9, 1, 0., 1., 5, co, 1e-7, buf, 1 << 40),
 ]
 where = ctypes.c_int()
 for device in (0, 1):
