@@ -129,6 +129,7 @@ class Solver:
     def __init__(self, device: int = 0):
         self.lib = load_library()
         self.device = device
+        self._types, self._gpu = None, f"cuda:{device}"
         stream_handle = None
         if device >= 0:
             import torch
@@ -406,29 +407,46 @@ class Solver:
                                                     G.shape[1], out.data_ptr()), "cadmm_op_wgrad_noalloc")
         return out
 
-    # products over groups of rows and orthogonalised updates: fp32, bf16 and fp16 device tensors of this solver's GPU
-    def _device_tensors(self, what, **tensors):
-        for name, t in tensors.items():
+    # Products over groups of rows and orthogonalised updates: fp32, bf16 and fp16 device tensors of this solver's GPU.  What a call
+    # asks of its tensors is one expression (a call of a small product is half host time); what is wrong is looked for afterwards.
+    def _value_types(self):
+        if self._types is None:
+            torch = self._torch
+            self._types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+        return self._types
+
+    def _on_raw_stream(self):
+        """_on_current_stream without a stream object."""
+        self.lib.cadmm_op_stream(self.h, self._torch._C._cuda_getCurrentRawStream(self.device))
+
+    def _refuse(self, what, types, rows, stacks):
+        """The reason why a call's tensors do not fit.  rows: (name, matrix with dense rows, shape or None, dtype or None); stacks:
+        (name, dense tensor, shape, dtypes)."""
+        for name, t, *_ in rows + stacks:
             if not t.is_cuda or t.device.index != self.device:
                 raise CadmmError(f"{what}: {name} is not on GPU {self.device}")
+        for name, t, shape, dtype in rows:
+            if t.dtype not in types or (dtype is not None and t.dtype != dtype):
+                raise CadmmError(f"{what}: {name} has type {t.dtype}")
+            if t.dim() != 2 or t.shape[1] < 1 or self._row_stride(t) is None:
+                raise CadmmError(f"{what}: {name} must be a matrix with dense rows")
+            if shape is not None and tuple(t.shape) != tuple(shape):
+                raise CadmmError(f"{what}: {name} must be {tuple(shape)}, not {tuple(t.shape)}")
+        for name, t, shape, dtypes in stacks:
+            if t.dtype not in dtypes:
+                raise CadmmError(f"{what}: {name} has type {t.dtype}")
+            if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+                raise CadmmError(f"{what}: {name} must be dense of shape {tuple(shape)}, not {tuple(t.shape)}")
+        raise CadmmError(f"{what}: the tensors do not fit together")
 
-    def _rows(self, what, name, t, types):
-        """Row stride of a matrix whose rows are dense."""
-        if t.dtype not in types:
-            raise CadmmError(f"{what}: {name} has type {t.dtype}")
-        if t.dim() != 2 or t.shape[1] < 1 or (t.shape[0] > 0 and t.shape[1] > 1 and t.stride(1) != 1):
-            raise CadmmError(f"{what}: {name} must be a matrix with dense rows")
-        return t.stride(0) if t.shape[0] > 1 else t.shape[1]
-
-    def _stack(self, what, name, t, shape, types):
-        if t.dtype not in types:
-            raise CadmmError(f"{what}: {name} has type {t.dtype}")
-        if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-            raise CadmmError(f"{what}: {name} must be dense of shape {tuple(shape)}")
-
-    def _value_types(self):
-        torch = self._torch
-        return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    @staticmethod
+    def _row_stride(t):
+        """Elements from one row of a matrix to the next; None if its rows are not dense."""
+        n, width = t.shape
+        if n > 1:
+            step, inner = t.stride()
+            return step if inner == 1 or width == 1 else None
+        return width if n == 0 or width == 1 or t.stride(1) == 1 else None
 
     def _scratch(self, query, *args):
         """Scratch of one call, from torch's allocator for the current stream: (aligned pointer, bytes, what keeps it alive)."""
@@ -436,7 +454,7 @@ class Solver:
         self._check(query(self.h, *args, C.byref(nbytes)), query.__name__)
         if nbytes.value == 0:
             return None, 0, None
-        hold = self._torch.empty(nbytes.value + 255, dtype=self._torch.uint8, device=f"cuda:{self.device}")
+        hold = self._torch.empty(nbytes.value + 255, dtype=self._torch.uint8, device=self._gpu)
         return (hold.data_ptr() + 255) & ~255, nbytes.value, hold
 
     def op_transform_grouped(self, A, B, group_ptr, transposed=False, out=None):
@@ -444,82 +462,98 @@ class Solver:
         (transposed: groups x C x K, and B_g is its transpose), group_ptr: int64 device tensor of groups + 1 bounds that do not
         descend.  `out` may be a preallocated n x C matrix with dense rows: rows of no group are left as they are there, and
         hold anything otherwise.  With the communities' weights in B: group_ptr = comm_row_ptr of get_graph."""
-        torch, what, types = self._torch, "op_transform_grouped", self._value_types()
-        self._device_tensors(what, A=A, B=B, group_ptr=group_ptr)
-        lda = self._rows(what, "A", A, types)
-        n, K = A.shape
-        groups = group_ptr.shape[0] - 1 if group_ptr.dim() == 1 else 0
-        if groups < 1:
-            raise CadmmError(f"{what}: group_ptr must hold groups + 1 bounds")
-        self._stack(what, "group_ptr", group_ptr, (groups + 1,), (torch.int64,))
-        width = B.shape[1 if transposed else 2] if B.dim() == 3 else 0
-        self._stack(what, "B", B, (groups, width, K) if transposed else (groups, K, width), (A.dtype,))
-        if out is None:
-            out = torch.empty((n, width), dtype=A.dtype, device=A.device)
-        self._device_tensors(what, out=out)
-        ldo = self._rows(what, "out", out, (A.dtype,))
-        if tuple(out.shape) != (n, width):
-            raise CadmmError(f"{what}: out must be {n} x {width}")
-        self._on_current_stream()
-        self._check(self.lib.cadmm_op_transform_grouped(self.h, types[A.dtype], A.data_ptr(), n, lda, K, B.data_ptr(), width,
-                                                        int(bool(transposed)), groups, group_ptr.data_ptr(), out.data_ptr(), ldo),
-                    "cadmm_op_transform_grouped")
+        torch, types, gpu = self._torch, self._types or self._value_types(), self.device
+        dtype = A.dtype
+        if A.dim() != 2 or B.dim() != 3 or group_ptr.dim() != 1 or group_ptr.shape[0] < 2:
+            raise CadmmError("op_transform_grouped: A is a matrix, B a stack of matrices, group_ptr holds groups + 1 bounds")
+        (n, K), (groups, rows, cols) = A.shape, B.shape
+        if transposed:
+            rows, cols = cols, rows
+        lda = self._row_stride(A)
+        fits = (dtype in types and K >= 1 and lda is not None and A.get_device() == gpu and B.get_device() == gpu and B.dtype == dtype and rows == K and
+                B.is_contiguous() and group_ptr.get_device() == gpu and group_ptr.dtype == torch.int64 and
+                group_ptr.shape[0] == groups + 1 and group_ptr.is_contiguous())
+        if fits and out is None:
+            out, ldo = torch.empty((n, cols), dtype=dtype, device=self._gpu), cols
+        elif fits and out.dim() == 2:
+            ldo = self._row_stride(out)
+            fits = out.dtype == dtype and out.get_device() == gpu and out.shape[0] == n and out.shape[1] == cols and ldo is not None
+        else:
+            fits = False
+        if not fits:
+            groups = group_ptr.shape[0] - 1
+            self._refuse("op_transform_grouped", types, [("A", A, None, None)] + ([] if out is None else [("out", out, (n, cols), dtype)]),
+                         [("group_ptr", group_ptr, (groups + 1,), (torch.int64,)), ("B", B, (groups, cols, K) if transposed else (groups, K, cols), (dtype,))])
+        self._on_raw_stream()
+        rc = self.lib.cadmm_op_transform_grouped(self.h, types[dtype], A.data_ptr(), n, lda, K, B.data_ptr(), cols, 1 if transposed else 0, groups,
+                                                 group_ptr.data_ptr(), out.data_ptr(), ldo)
+        if rc:
+            self._check(rc, "cadmm_op_transform_grouped")
         return out
 
     def op_wgrad_grouped(self, A, G, group_ptr, out=None, out_dtype=None):
         """out[g] = A_g^T G_g over the rows of every group (groups x K x C): the gradient of op_transform_grouped with respect to
         B.  In fp32 unless `out` or out_dtype (fp32 or the operands' type) says otherwise; zeros for a group without rows."""
-        torch, what, types = self._torch, "op_wgrad_grouped", self._value_types()
-        self._device_tensors(what, A=A, G=G, group_ptr=group_ptr)
-        lda, ldg = self._rows(what, "A", A, types), self._rows(what, "G", G, (A.dtype,))
-        if A.shape[0] != G.shape[0]:
-            raise CadmmError(f"{what}: A and G have different numbers of rows")
-        groups = group_ptr.shape[0] - 1 if group_ptr.dim() == 1 else 0
-        if groups < 1:
-            raise CadmmError(f"{what}: group_ptr must hold groups + 1 bounds")
-        self._stack(what, "group_ptr", group_ptr, (groups + 1,), (torch.int64,))
-        (n, K), width = A.shape, G.shape[1]
-        if out is None:
-            out = torch.empty((groups, K, width), dtype=out_dtype or torch.float32, device=A.device)
-        self._device_tensors(what, out=out)
-        self._stack(what, "out", out, (groups, K, width), (torch.float32, A.dtype) if out_dtype is None else (out_dtype,))
+        torch, types, gpu = self._torch, self._types or self._value_types(), self.device
+        dtype = A.dtype
+        if A.dim() != 2 or G.dim() != 2 or group_ptr.dim() != 1 or group_ptr.shape[0] < 2:
+            raise CadmmError("op_wgrad_grouped: A and G are matrices, group_ptr holds groups + 1 bounds")
+        (n, K), (m, width), groups = A.shape, G.shape, group_ptr.shape[0] - 1
+        lda, ldg = self._row_stride(A), self._row_stride(G)
+        wanted = (torch.float32, dtype) if out_dtype is None else (out_dtype,)
+        fits = (dtype in types and G.dtype == dtype and m == n and K >= 1 and width >= 1 and lda is not None and ldg is not None and
+                A.get_device() == gpu and G.get_device() == gpu and group_ptr.get_device() == gpu and group_ptr.dtype == torch.int64 and
+                group_ptr.is_contiguous() and (out_dtype is None or out_dtype == torch.float32 or out_dtype == dtype))
+        if fits and out is None:
+            out = torch.empty((groups, K, width), dtype=out_dtype or torch.float32, device=self._gpu)
+        elif fits:
+            fits = out.dtype in wanted and out.get_device() == gpu and tuple(out.shape) == (groups, K, width) and out.is_contiguous()
+        if not fits:
+            self._refuse("op_wgrad_grouped", types, [("A", A, None, None), ("G", G, (n, width), dtype)],
+                         [("group_ptr", group_ptr, (groups + 1,), (torch.int64,))] + ([] if out is None else [("out", out, (groups, K, width), wanted)]))
         ptr, nbytes, hold = self._scratch(self.lib.cadmm_op_wgrad_grouped_scratch, n, K, width, groups)
-        self._on_current_stream()
-        self._check(self.lib.cadmm_op_wgrad_grouped(self.h, types[A.dtype], A.data_ptr(), n, lda, K, G.data_ptr(), ldg, width, groups,
-                                                    group_ptr.data_ptr(), types.get(out.dtype, -1), out.data_ptr(), ptr, nbytes),
-                    "cadmm_op_wgrad_grouped")
+        self._on_raw_stream()
+        rc = self.lib.cadmm_op_wgrad_grouped(self.h, types[dtype], A.data_ptr(), n, lda, K, G.data_ptr(), ldg, width, groups,
+                                             group_ptr.data_ptr(), types[out.dtype], out.data_ptr(), ptr, nbytes)
+        if rc:
+            self._check(rc, "cadmm_op_wgrad_grouped")
         return out
 
     def op_orthogonalise(self, G, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, out=None):
         """G (K x C, or a stack batch x K x C) with the singular values of every matrix brought towards one: `steps` times
         X <- a X + (b S + c S^2) X, S = X X^T, from X = G / (||G||_F + eps).  `out` may be G itself."""
-        torch, what, types = self._torch, "op_orthogonalise", self._value_types()
-        out = torch.empty_like(G, memory_format=torch.contiguous_format) if out is None else out
-        self._device_tensors(what, G=G, out=out)
-        batch, K, width = self._matrices(what, G)
-        self._stack(what, "G", G, G.shape, types)
-        self._stack(what, "out", out, G.shape, (G.dtype,))
+        types, shape = self._types or self._value_types(), G.shape
+        batch, K, width = self._matrices("op_orthogonalise", G)
+        fits = G.dtype in types and G.get_device() == self.device and G.is_contiguous()
+        if fits and out is None:
+            out = self._torch.empty(shape, dtype=G.dtype, device=self._gpu)
+        elif fits:
+            fits = out.dtype == G.dtype and out.get_device() == self.device and out.shape == shape and out.is_contiguous()
+        if not fits:
+            self._refuse("op_orthogonalise", types, [], [("G", G, shape, types)] + ([] if out is None else [("out", out, shape, (G.dtype,))]))
         ptr, nbytes, hold = self._scratch(self.lib.cadmm_op_orthogonalise_scratch, batch, K, width)
-        self._on_current_stream()
-        self._check(self.lib.cadmm_op_orthogonalise(self.h, types[G.dtype], G.data_ptr(), batch, K, width, steps, self._coefficients(coefficients),
-                                                    eps, out.data_ptr(), ptr, nbytes), "cadmm_op_orthogonalise")
+        self._on_raw_stream()
+        rc = self.lib.cadmm_op_orthogonalise(self.h, types[G.dtype], G.data_ptr(), batch, K, width, steps, self._coefficients(coefficients), eps,
+                                             out.data_ptr(), ptr, nbytes)
+        if rc:
+            self._check(rc, "cadmm_op_orthogonalise")
         return out
 
     def op_muon_step(self, W, M, G, *, lr, momentum=0.95, nesterov=True, weight_decay=0.0, scale=1.0, steps=5,
                      coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7):
         """One optimiser step on W (K x C, or a stack), in place: M <- momentum M + G, D = G + momentum M (nesterov) or M,
         W <- (1 - lr weight_decay) W - lr scale O with O the orthogonalised D.  W and M are fp32."""
-        torch, what, types = self._torch, "op_muon_step", self._value_types()
-        self._device_tensors(what, W=W, M=M, G=G)
-        batch, K, width = self._matrices(what, G)
-        self._stack(what, "G", G, G.shape, types)
-        self._stack(what, "W", W, G.shape, (torch.float32,))
-        self._stack(what, "M", M, G.shape, (torch.float32,))
+        types, shape, f32, gpu = self._types or self._value_types(), G.shape, self._torch.float32, self.device
+        batch, K, width = self._matrices("op_muon_step", G)
+        if not (G.dtype in types and G.get_device() == gpu and G.is_contiguous() and W.dtype == f32 and W.get_device() == gpu and W.shape == shape and
+                W.is_contiguous() and M.dtype == f32 and M.get_device() == gpu and M.shape == shape and M.is_contiguous()):
+            self._refuse("op_muon_step", types, [], [("G", G, shape, types), ("W", W, shape, (f32,)), ("M", M, shape, (f32,))])
         ptr, nbytes, hold = self._scratch(self.lib.cadmm_op_orthogonalise_scratch, batch, K, width)
-        self._on_current_stream()
-        self._check(self.lib.cadmm_op_muon_step(self.h, types[G.dtype], G.data_ptr(), W.data_ptr(), M.data_ptr(), batch, K, width, lr, momentum,
-                                                int(bool(nesterov)), weight_decay, scale, steps, self._coefficients(coefficients), eps, ptr, nbytes),
-                    "cadmm_op_muon_step")
+        self._on_raw_stream()
+        rc = self.lib.cadmm_op_muon_step(self.h, types[G.dtype], G.data_ptr(), W.data_ptr(), M.data_ptr(), batch, K, width, lr, momentum,
+                                         1 if nesterov else 0, weight_decay, scale, steps, self._coefficients(coefficients), eps, ptr, nbytes)
+        if rc:
+            self._check(rc, "cadmm_op_muon_step")
 
     def _coefficients(self, coefficients):
         if len(coefficients) != 3:

@@ -354,19 +354,19 @@ __global__ __launch_bounds__(1024) void orthogonal_block_kernel(Source<T> src, c
     const int xi = wave / CT, xj = wave % CT;                                                 // of X
     const bool holds = 32 * ti < r && 32 * tj < r;                             // (all else is zeros)
     floatx16 acc;
-    // (parts in the accumulators' order: 16 numbers of a lane, lanes of a tile, tiles)
+    // (parts: four numbers of a lane next to those of the other lanes, four such of a tile)
     auto load_sum = [&](const float* from) {
         floatx16 v;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const float4 f = *reinterpret_cast<const float4*>(from + (tile * 64 + lane) * 16 + 4 * q);
+            const float4 f = *reinterpret_cast<const float4*>(from + ((tile * 4 + q) * 64 + lane) * 4);
             v[4 * q] = f.x; v[4 * q + 1] = f.y; v[4 * q + 2] = f.z; v[4 * q + 3] = f.w;
         }
         return v;
     };
     auto store_sum = [&](float* to, const floatx16& v) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) *reinterpret_cast<float4*>(to + (tile * 64 + lane) * 16 + 4 * q) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+        for (int q = 0; q < 4; ++q) *reinterpret_cast<float4*>(to + ((tile * 4 + q) * 64 + lane) * 4) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
     };
     auto own_square = [&] {                                                    // this group's part of the slab's part of S
         __syncthreads();
