@@ -56,7 +56,7 @@ __device__ __forceinline__ void place(unsigned tiles, bool slices, int64_t& slot
 }
 
 template <class P, class T, Lie YL>
-__global__ __launch_bounds__(P::THREADS, P::THREADS == 256 ? 2 : 1) void grouped_nn_kernel(
+__global__ __launch_bounds__(P::THREADS, P::THREADS <= 256 ? 2 : 1) void grouped_nn_kernel(
     const T* __restrict__ A, int64_t n, int64_t lda, int K, const T* __restrict__ B, int C, int groups, const int64_t* __restrict__ ptr,
     T* __restrict__ out, int64_t ldo, int col_tiles, int slices, int whole_out) {
     __shared__ __align__(16) unsigned short S[P::kLds];
@@ -86,7 +86,7 @@ __device__ __forceinline__ int64_t part_place(int64_t lo, int64_t hi, int64_t mo
 }
 
 template <class P, class T, class O>
-__global__ __launch_bounds__(P::THREADS, P::THREADS == 256 ? 2 : 1) void grouped_tn_kernel(
+__global__ __launch_bounds__(P::THREADS, P::THREADS <= 256 ? 2 : 1) void grouped_tn_kernel(
     const T* __restrict__ A, int64_t n, int64_t lda, int K, const T* __restrict__ G, int64_t ldg, int C, int groups,
     const int64_t* __restrict__ ptr, O* __restrict__ out, float* __restrict__ partial, int64_t most, int64_t part_size, int col_tiles, int tiles,
     int slices, int whole_out) {
@@ -150,26 +150,41 @@ void with_type(int type, F f) {
 //           256 x 256 202 us, 128 x 256 214 (16384 x 2048 x 1024, 64 groups).
 //   kMiddle 128 x 128;  kSmall 64 x 64, where larger ones would not give every compute unit one
 //   kFew    32 x 64, for groups of a few rows: reading the weights is all there is to it, from many places and far ahead.
+//   kLone.. the same tiles, with more sets of wavefronts to share the contraction, where that leaves no compute unit a second workgroup
+//           anyway.  fp32: one row of 512 x 512 15.9 -> 8.5 us, 16 rows through 16 x 2048 x 1024 71 -> 56, but 64 rows through 64 of them
+//           103 -> 125; 300 x 1000 x 1000 in 4 groups 25.7 -> 22.4, but 100000 x 64 x 64 16.5 -> 28.
 template <class T> constexpr int kStep = 128 / sizeof(T);
-enum Size { kLarge, kMiddle, kSmall, kFew };
+enum Size { kLarge, kMiddle, kSmall, kFew, kLoneSmall, kLoneFew };
 template <class T, Lie X, Lie Y, Mode M, bool STRAIGHT = sizeof(T) == 2 && M == kWhole>
 struct Sizes {
     using Large = Product<T, X, Y, M, 2, 2, 2, 4, kStep<T> / 2, 1, 1>;
     using Middle = Product<T, X, Y, M, 2, 2, 2, 2, kStep<T>, 1, 1>;
     using Small = Product<T, X, Y, M, 2, 2, 1, 1, kStep<T>, 2, 2>;
     using Few = Product<T, X, Y, M, 1, 2, 1, 1, kStep<T>, 4, 2>;
+    using LoneSmall = Product<T, X, Y, M, 2, 2, 1, 1, kStep<T>, 1, 2, 2>;
+    using LoneFew = Product<T, X, Y, M, 1, 2, 1, 1, kStep<T>, 2, 2, 4>;
 };
 template <class T, Lie X, Lie Y, Mode M>
 struct Sizes<T, X, Y, M, true> {
     using Large = std::conditional_t<X == kAlong, Direct<T, X, Y, 2, 2, 2, 4, 3, 1, 32>, Direct<T, X, Y, 2, 4, 4, 2, 2>>;
     using Middle = Direct<T, X, Y, 2, 2, 2, 2, 2>;
     using Small = Direct<T, X, Y, 2, 2, 1, 1, 4>;
-    using Few = Direct<T, X, Y, 1, 2, 1, 1, 6, 2>;
+    using Few = Direct<T, X, Y, 1, 2, 1, 1, 3, 4>;             // (64 rows through 64 x 2048 x 1024: 64 us, with two sets 72)
+    using LoneSmall = Direct<T, X, Y, 2, 2, 1, 1, 2, 4>;
+    using LoneFew = Few;
 };
+template <Size SIZE, class S>
+auto sized() {
+    if constexpr (SIZE == kLarge) return (typename S::Large*)nullptr;
+    else if constexpr (SIZE == kMiddle) return (typename S::Middle*)nullptr;
+    else if constexpr (SIZE == kSmall) return (typename S::Small*)nullptr;
+    else if constexpr (SIZE == kFew) return (typename S::Few*)nullptr;
+    else if constexpr (SIZE == kLoneSmall) return (typename S::LoneSmall*)nullptr;
+    else return (typename S::LoneFew*)nullptr;
+}
 template <Size SIZE, class T, Lie X, Lie Y, Mode M>
-using Sized = std::conditional_t<SIZE == kLarge, typename Sizes<T, X, Y, M>::Large, std::conditional_t<SIZE == kMiddle, typename Sizes<T, X, Y, M>::Middle,
-              std::conditional_t<SIZE == kSmall, typename Sizes<T, X, Y, M>::Small, typename Sizes<T, X, Y, M>::Few>>>;
-constexpr int kSizeCols[] = {256, 128, 64, 64}, kNnRows[] = {128, 128, 64, 32};
+using Sized = std::remove_pointer_t<decltype(sized<SIZE, Sizes<T, X, Y, M>>())>;
+constexpr int kSizeCols[] = {256, 128, 64, 64, 64, 64}, kNnRows[] = {128, 128, 64, 32, 64, 32};
 int tn_rows(Size s, bool straight) { return s == kLarge ? straight ? 256 : 128 : kNnRows[s]; }
 constexpr int64_t kCus = 256;
 
@@ -183,7 +198,9 @@ Size nn_size(int64_t n, int C, int groups, bool straight) {
         const bool fits = C > kSizeCols[s] / 2 && rows > kNnRows[s] / 2;
         if (fits && (n / kNnRows[s] + hit / 2) * over(C, kSizeCols[s]) >= kCus) return s;
     }
-    return rows > 32 ? kSmall : kFew;
+    const Size s = rows > 32 ? kSmall : kFew;
+    const int64_t tiles = (n / kNnRows[s] + hit) * over(C, kSizeCols[s]);
+    return s == kSmall ? tiles <= kCus ? kLoneSmall : s : tiles <= 2 * kCus ? kLoneFew : s;
 }
 
 struct TnPlan { Size size; int64_t most, parts; };
@@ -199,6 +216,7 @@ TnPlan tn_plan(int64_t n, int K, int C, int groups, bool straight) {
         if (s == kLarge && share < 512) continue;
         if (tiles * groups < 2 * kCus * 2) p.most = std::max<int64_t>(256, over(share, 64) * 64);
         p.parts = p.most < n ? 2 * (n / p.most + 1) : 0;
+        if (s == kSmall && (n / p.most + groups) * tiles <= kCus) p.size = kLoneSmall;
         return p;
     }
     return {};
@@ -220,7 +238,9 @@ void nn_launch(hipStream_t s, const GroupedNN& a, Size size, bool whole_out) {
         if constexpr (sizeof(T) == 2 && MODE == kWhole) go(std::integral_constant<Size, kLarge>());
     } else if (size == kMiddle) go(std::integral_constant<Size, kMiddle>());
     else if (size == kSmall) go(std::integral_constant<Size, kSmall>());
-    else go(std::integral_constant<Size, kFew>());
+    else if (size == kFew) go(std::integral_constant<Size, kFew>());
+    else if (size == kLoneSmall) go(std::integral_constant<Size, kLoneSmall>());
+    else go(std::integral_constant<Size, kLoneFew>());
 }
 
 template <class T, Mode MODE, class O>
@@ -237,7 +257,8 @@ void tn_launch(hipStream_t s, const GroupedTN& a, const TnPlan& plan) {
     };
     if (plan.size == kLarge) go(std::integral_constant<Size, kLarge>());
     else if (plan.size == kMiddle) go(std::integral_constant<Size, kMiddle>());
-    else go(std::integral_constant<Size, kSmall>());
+    else if (plan.size == kSmall) go(std::integral_constant<Size, kSmall>());
+    else go(std::integral_constant<Size, kLoneSmall>());
     if (plan.parts > 0) {
         const unsigned bx = (unsigned)std::min<int64_t>(over(count, 1024), std::max<int64_t>(1, 8 * kCus / a.groups));
         for (int g0 = 0; g0 < a.groups; g0 += 65535)       // (a grid's second dimension)

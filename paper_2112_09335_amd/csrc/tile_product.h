@@ -138,8 +138,8 @@ __device__ __forceinline__ int along_swizzle(int chunk) { return (chunk & 3) << 
 template <int ROWS>
 __device__ __forceinline__ int across_swizzle(int k) { return ROWS >= 128 ? (k & 3) << 2 : ROWS == 64 ? (k & 2) << 1 : 0; }
 
-// One operand's tile: ROWS rows (i) by BK of the contraction, carried by THREADS threads.
-template <class T, Lie LIE, Mode MODE, int ROWS, int BK, int THREADS, int PF>
+// One operand's tile: ROWS rows (i) by BK of the contraction, carried by THREADS threads (of a set of wavefronts).
+template <class T, Lie LIE, Mode MODE, int ROWS, int BK, int THREADS, int PF, int WK>
 struct Operand {
     using E = typename View<T>::Element;
     static constexpr int kParts_ = kParts<T>;
@@ -154,17 +154,18 @@ struct Operand {
     unsigned place[kEach];                                               // kWhole: bytes from the tile's (kAlong) or the step's (kAcross) first
     const E* at[kEach];                                                  // kAny: start of the row (kAlong), or of the row of the step (kAcross)
 
-    __device__ __forceinline__ static int row_of(int u) { return (threadIdx.x + u * THREADS) / kPerRow; }
-    __device__ __forceinline__ static int chunk_of(int u) { return (threadIdx.x + u * THREADS) % kPerRow; }
-    __device__ __forceinline__ static bool carries(int u) { return !kIdle || (int)threadIdx.x + u * THREADS < kChunks; }
+    __device__ __forceinline__ static int thread() { return threadIdx.x % THREADS; }
+    __device__ __forceinline__ static int row_of(int u) { return (thread() + u * THREADS) / kPerRow; }
+    __device__ __forceinline__ static int chunk_of(int u) { return (thread() + u * THREADS) % kPerRow; }
+    __device__ __forceinline__ static bool carries(int u) { return !kIdle || thread() + u * THREADS < kChunks; }
 
-    __device__ __forceinline__ void begin(const View<T>& x) {
+    __device__ __forceinline__ void begin(const View<T>& x, int64_t from) {     // from: where the set's first step begins
 #pragma unroll
         for (int u = 0; u < kEach; ++u) {
             int r = row_of(u);
             if (LIE == kAlong && r >= x.rows) r = x.rows - 1;               // rows past the end: any (their results are not stored)
             if constexpr (MODE == kWhole) place[u] = (unsigned)r * (unsigned)(x.ld * sizeof(E)) + chunk_of(u) * kChunkBytes;
-            else at[u] = x.p + (int64_t)r * x.ld;
+            else at[u] = x.p + ((LIE == kAcross ? from : 0) + r) * x.ld;
         }
     }
     // the step that begins at k0, into slot s
@@ -187,7 +188,7 @@ struct Operand {
                 if constexpr (LIE == kAlong) fetch_any<T>(q[s][u], at[u], (int)k0 + 8 * chunk_of(u), (int)x.depth);
                 else {
                     fetch_any<T>(q[s][u], row_of(u) < left ? at[u] : x.p, 8 * chunk_of(u), x.rows);          // (row 0 of the view is there)
-                    at[u] += BK * x.ld;
+                    at[u] += WK * BK * x.ld;
                 }
             }
         }
@@ -274,6 +275,32 @@ struct Tile {
                 for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
     }
 
+    // The sets' sums, to the first set; the LDS is free before, and behind the slabs not after.
+    static constexpr int kSums = kSlabs + (WK - 1) * BM * BN * 2;          // in 16-bit elements
+    __device__ __forceinline__ static void join(floatx16 (&acc)[TM][TN], unsigned short* lds) {
+        if constexpr (WK > 1) {
+            const int set = (threadIdx.x >> 6) / (WM * WN);
+            float4* sums = reinterpret_cast<float4*>(lds + kSlabs) + threadIdx.x % (64 * WM * WN);
+            constexpr int EACH = 64 * WM * WN;                                // (of a set's lanes, a quad of results next to the other lanes')
+            if (set > 0)
+#pragma unroll
+                for (int q = 0; q < TM * TN * 4; ++q) {
+                    const floatx16& v = acc[q / 4 / TN][q / 4 % TN];
+                    sums[((set - 1) * TM * TN * 4 + q) * EACH] = make_float4(v[q % 4 * 4], v[q % 4 * 4 + 1], v[q % 4 * 4 + 2], v[q % 4 * 4 + 3]);
+                }
+            __syncthreads();
+            if (set == 0)
+#pragma unroll
+                for (int t = 0; t < WK - 1; ++t)
+#pragma unroll
+                    for (int q = 0; q < TM * TN * 4; ++q) {
+                        const float4 u = sums[(t * TM * TN * 4 + q) * EACH];
+                        floatx16& v = acc[q / 4 / TN][q / 4 % TN];
+                        v[q % 4 * 4] += u.x; v[q % 4 * 4 + 1] += u.y; v[q % 4 * 4 + 2] += u.z; v[q % 4 * 4 + 3] += u.w;
+                    }
+        }
+    }
+
     // f(row, column, four results) for every quad of the tile, 16 (TN >= 2) or 8 neighbouring lanes along a row.  Every wavefront passes
     // its results through LDS of its own.  MIRROR: what f returns goes on to m(column, row, four results of neighbouring rows).
     template <bool MIRROR, class F, class M>
@@ -323,19 +350,19 @@ struct Tile {
 };
 
 // Tiles whose operands go through registers: any operand, any rows.
-template <class T, Lie XL, Lie YL, Mode MODE, int WM_, int WN_, int TM_, int TN_, int BK_, int PF_, int BUFFERS_>
-struct Product : Tile<WM_, WN_, TM_, TN_> {
-    using Base = Tile<WM_, WN_, TM_, TN_>;
-    using Base::WM; using Base::WN; using Base::TM; using Base::TN; using Base::BM; using Base::BN; using Base::THREADS; using Base::kSlabs;
+template <class T, Lie XL, Lie YL, Mode MODE, int WM_, int WN_, int TM_, int TN_, int BK_, int PF_, int BUFFERS_, int WK_ = 1>
+struct Product : Tile<WM_, WN_, TM_, TN_, WK_> {
+    using Base = Tile<WM_, WN_, TM_, TN_, WK_>;
+    using Base::WM; using Base::WN; using Base::TM; using Base::TN; using Base::WK; using Base::BM; using Base::BN; using Base::THREADS; using Base::kSlabs;
     static constexpr int BK = BK_, PF = PF_, BUFFERS = BUFFERS_;
-    using X = Operand<T, XL, MODE, BM, BK, THREADS, PF>;
-    using Y = Operand<T, YL, MODE, BN, BK, THREADS, PF>;
+    using X = Operand<T, XL, MODE, BM, BK, 64 * WM * WN, PF, WK>;
+    using Y = Operand<T, YL, MODE, BN, BK, 64 * WM * WN, PF, WK>;
     static constexpr int P = kParts<T>;
     static constexpr int kBuffer = X::kSize + Y::kSize;
-    static constexpr int kLds = BUFFERS * kBuffer > kSlabs ? BUFFERS * kBuffer : kSlabs;
+    static constexpr int kLds = WK * BUFFERS * kBuffer > Base::kSums ? WK * BUFFERS * kBuffer : Base::kSums;
 
     __device__ __forceinline__ static void step(floatx16 (&acc)[TM][TN], const unsigned short* S) {
-        const int wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
+        const int wave = (threadIdx.x >> 6) % (WM * WN), wm = wave / WN, wn = wave % WN;
 #pragma unroll
         for (int s = 0; s < BK / 16; ++s) {
             uintx4 a[P][TM];
@@ -364,44 +391,46 @@ struct Product : Tile<WM_, WN_, TM_, TN_> {
         Base::clear(acc);
         const int64_t depth = x.depth;
         if (depth <= 0) return;
+        const int set = WK > 1 ? __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) / (WM * WN)) : 0;
+        const int64_t from = set * BK;
+        S += set * BUFFERS * kBuffer;
         X X_;
         Y Y_;
-        X_.begin(x);
-        Y_.begin(y);
+        X_.begin(x, from);
+        Y_.begin(y, from);
 #pragma unroll
-        for (int s = 0; s < PF; ++s)
-        { X_.load(x, s * BK, s); Y_.load(y, s * BK, s); }
+        for (int s = 0; s < PF; ++s) { X_.load(x, from + s * WK * BK, s); Y_.load(y, from + s * WK * BK, s); }
         // (steps past the end load what is there and store zeros: a load or store that some steps leave out would make every wait
         // for loads one for all of them, whatever is ahead)
         int buffer = 0;
         if constexpr (BUFFERS == 2) {
-            X_.store(x, 0, 0, S);
-            Y_.store(y, 0, 0, S + X::kSize);
+            X_.store(x, from, 0, S);
+            Y_.store(y, from, 0, S + X::kSize);
             __syncthreads();
         }
-        for (int64_t k0 = 0; k0 < depth; k0 += PF * BK) {
+        for (int64_t k0 = 0; k0 < depth; k0 += PF * WK * BK) {
 #pragma unroll
             for (int u = 0; u < PF; ++u) {
-                const int64_t k = k0 + u * BK;
-                if (u > 0 && k >= depth) break;                          // (uniform)
+                const int64_t k = k0 + u * WK * BK;
+                if (u > 0 && k >= depth) break;                          // (uniform, for all sets)
                 if constexpr (BUFFERS == 1) {
-                    X_.store(x, k, u, S);
-                    Y_.store(y, k, u, S + X::kSize);
+                    X_.store(x, from + k, u, S);
+                    Y_.store(y, from + k, u, S + X::kSize);
                     __syncthreads();
                 }
-                X_.load(x, k + PF * BK, u);
-                Y_.load(y, k + PF * BK, u);
+                X_.load(x, from + k + PF * WK * BK, u);
+                Y_.load(y, from + k + PF * WK * BK, u);
                 step(acc, S + buffer * kBuffer);
                 if constexpr (BUFFERS == 2) {
                     buffer ^= 1;
-                    X_.store(x, k + BK, (u + 1) % PF, S + buffer * kBuffer);
-                    Y_.store(y, k + BK, (u + 1) % PF, S + buffer * kBuffer + X::kSize);
+                    X_.store(x, from + k + WK * BK, (u + 1) % PF, S + buffer * kBuffer);
+                    Y_.store(y, from + k + WK * BK, (u + 1) % PF, S + buffer * kBuffer + X::kSize);
                 }
                 __syncthreads();
             }
         }
+        Base::join(acc, S - set * BUFFERS * kBuffer);
     }
-
 };
 
 // Tiles whose operands go from memory straight to LDS, STAGES - 1 steps ahead: bf16, fp16 and Pairs whose chunks are whole.  An LDS tile
@@ -488,8 +517,7 @@ struct Direct : Tile<WM_, WN_, TM_, TN_, WK_> {
     using Y = DirectOperand<T, YL, BN, BK, WM * WN>;
     static constexpr int kStage = X::kSize + Y::kSize;
     static constexpr int kSet = STAGES * kStage;                              // bytes of a set of wavefronts
-    static constexpr int kSums = (WK - 1) * BM * BN * 4 + 2 * kSlabs;          // what the sets leave each other, behind the slabs
-    static constexpr int kLds = (WK * kSet > kSums ? WK * kSet : kSums) / 2;     // in 16-bit elements
+    static constexpr int kLds = WK * kSet / 2 > Base::kSums ? WK * kSet / 2 : Base::kSums;     // in 16-bit elements
     static constexpr int kAhead = (STAGES - 2) * (X::kEach + Y::kEach);      // loads that may be on their way when the next step begins
 
     struct Operands { uintx4 a[P][TM], b[P][TN]; };
@@ -559,26 +587,7 @@ struct Direct : Tile<WM_, WN_, TM_, TN_, WK_> {
             add(acc, f[(SUBS - 1) & 1]);
         }
         meet<0>();                                                            // the LDS is free
-        if constexpr (WK > 1) {
-            float4* sums = reinterpret_cast<float4*>(lds + kSlabs) + threadIdx.x % (64 * WM * WN);
-            constexpr int EACH = 64 * WM * WN;                                // (of a set's lanes, a quad of results next to the other lanes')
-            if (set > 0)
-#pragma unroll
-                for (int q = 0; q < TM * TN * 4; ++q) {
-                    const floatx16& v = acc[q / 4 / TN][q / 4 % TN];
-                    sums[((set - 1) * TM * TN * 4 + q) * EACH] = make_float4(v[q % 4 * 4], v[q % 4 * 4 + 1], v[q % 4 * 4 + 2], v[q % 4 * 4 + 3]);
-                }
-            meet<0>();
-            if (set == 0)
-#pragma unroll
-                for (int t = 0; t < WK - 1; ++t)
-#pragma unroll
-                    for (int q = 0; q < TM * TN * 4; ++q) {
-                        const float4 u = sums[(t * TM * TN * 4 + q) * EACH];
-                        floatx16& v = acc[q / 4 / TN][q / 4 % TN];
-                        v[q % 4 * 4] += u.x; v[q % 4 * 4 + 1] += u.y; v[q % 4 * 4 + 2] += u.z; v[q % 4 * 4 + 3] += u.w;
-                    }
-        }
+        Base::join(acc, lds);
     }
 };
 
