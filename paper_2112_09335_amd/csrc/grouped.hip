@@ -110,7 +110,7 @@ __global__ __launch_bounds__(P::THREADS, P::THREADS <= 256 ? 2 : 1) void grouped
     } else {
         O* to = out + (int64_t)g * K * C;
         P::drain(acc, S, [&](int row, int col, float4 v) {
-            if (i0 + row < K && c0 + col < C) put(to + (int64_t)(i0 + row) * C, c0 + col, C, v, whole_out);
+            if (i0 + row < K && c0 + col < C) put<true>(to + (int64_t)(i0 + row) * C, c0 + col, C, v, whole_out);
         });
     }
 }
