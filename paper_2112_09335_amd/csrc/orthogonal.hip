@@ -233,8 +233,8 @@ __global__ __launch_bounds__(P::THREADS, P::THREADS == 256 ? 2 : 1) void orthogo
 }
 
 // Matrices with at most 32 RT (64 or 128) rows on the smaller side.  A workgroup of sixteen wavefronts holds X, that is a slab of up to
-// 16384 / RT / 32 of its columns, and S, then P, in LDS; with one slab the whole polynomial is one launch (256 x 64: fifteen products
-// in 95 us as launches of their own).  With more, a launch per step: every workgroup adds up the slabs' parts of S, forms P itself, applies
+// 16384 / RT / 32 of its columns, and S, then P, in LDS; with one slab the whole polynomial is one launch (256 x 64 fp32: 36 us, and 95
+// with its fifteen products as launches of their own); what bounds it is one compute unit's LDS and six barriers a step.  With more, a launch per step: every workgroup adds up the slabs' parts of S, forms P itself, applies
 // it to its slab and leaves its part of the next S.  X lies as its smaller side's rows, whichever way the matrix lies.
 constexpr int kMostSteps = 64;
 struct Schedule { float s[kMostSteps], p2[kMostSteps], p1[kMostSteps], p0[kMostSteps], x[kMostSteps]; };      // factors of S, S^2, S, 1 and of X' a step
