@@ -522,12 +522,13 @@ double polynomial_bound(double a, double b, double c, double s) {
     auto see = [&](double x2) {                        // where the derivative a + 3 b x^2 + 5 c x^4 is zero
         if (x2 > 0.0 && x2 < s * s) most = std::max(most, f(std::sqrt(x2)));
     };
+    // its roots in x^2 are q / (5 c) and a / q: the sum in q has terms of one sign, so that neither root is lost to cancellation however small
+    // c is next to b (with c = 0 the first is no number or none in the range, with b = 0 too both are; q = 0: a or c is zero then, x^2 = 0)
     const double d = 9.0 * b * b - 20.0 * a * c;
-    if (c != 0.0 && d >= 0.0) {
-        see((-3.0 * b + std::sqrt(d)) / (10.0 * c));
-        see((-3.0 * b - std::sqrt(d)) / (10.0 * c));
-    } else if (c == 0.0 && b != 0.0) {
-        see(-a / (3.0 * b));
+    if (d >= 0.0) {
+        const double q = -0.5 * (3.0 * b + std::copysign(std::sqrt(d), b));
+        see(q / (5.0 * c));
+        see(a / q);
     }
     return std::isfinite(most) && std::isfinite(f(s)) ? most : HUGE_VAL;
 }

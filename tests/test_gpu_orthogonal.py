@@ -102,6 +102,15 @@ def test_other_polynomials(solver, coefficients, steps, batch, K, width):
     check(solver.op_orthogonalise(G.cuda(), steps=steps, coefficients=coefficients).cpu(), G, "f32", steps, coefficients)
 
 
+@pytest.mark.parametrize("c", [0.0, 1e-17, -1e-17, 1e-16, 1e-9])
+@pytest.mark.parametrize("batch,K,width", [(2, 48, 80), (1, 260, 130), (1, 128, 512)])
+def test_a_fifth_power_that_hardly_counts(solver, c, batch, K, width):
+    """What the iterates are scaled by follows from the polynomial's largest value, which lies inside [0, 1] here."""
+    import torch
+    G = gradient(torch, 6, batch, K, width, "f32")
+    check(solver.op_orthogonalise(G.cuda(), steps=2, coefficients=(3.0, -3.0, c)).cpu(), G, "f32", 2, (3.0, -3.0, c))
+
+
 def test_singular_values_come_near_one(solver):
     """Fifteen steps of the cubic polynomial leave an orthogonal matrix: X X^T = 1 to the products' accuracy."""
     import torch

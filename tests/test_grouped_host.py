@@ -1,6 +1,7 @@
 """Refusals of the products over groups of rows and of the orthogonalised updates, and the streams and devices they use: no GPU call."""
 import ctypes as C
 
+import numpy as np
 import pytest
 
 from paper_2112_09335_amd import binding
@@ -152,3 +153,22 @@ for device in (0, 1):
                 assert not any(w == "record-elsewhere" for w, _, _ in log), log
                 assert rec.hipGetDevice(ctypes.byref(where)) == 0 and where.value == device
 """)
+
+
+def most_of(coefficients):
+    """The largest |x (a + b x^2 + c x^4)| on [0, 1], by looking at a million of them (flat around it: off by 1e-11 of a + |b| + |c|)."""
+    a, b, c = (np.float64(np.float32(x)) for x in coefficients)
+    x = np.linspace(0.0, 1.0, 1 << 20)
+    return np.abs(x * (a + x * x * (b + c * x * x))).max()
+
+
+@pytest.mark.parametrize("call", [ortho, muon])
+@pytest.mark.parametrize("shape", [(3, -3, 1e-17), (3, -3, -1e-17), (3, -3, 1e-18), (3, -3, 1e-16), (3, -3, 0), (3, -3, 1e-9), (-3, 3, 1e-17), (3, -3, 1e-3), (1, 0, -1),
+                                   (-1, 0, 1), (5, -20, 16), (0, 1, -1), (0, 1, 1e-20), (1, -1e-20, -1), (3, -4, 1.2), (1, 1, 1), (1e-3, -1, 1e-17)])
+def test_growth_is_judged_by_the_largest_value_wherever_it_lies(host, call, shape):
+    """One step, coefficients brought to where the largest value is just below or above 1024, whatever their sizes relative to each other."""
+    for size, code in ((1023.0, EUNSUPPORTED), (1025.0, EINVAL)):            # (EUNSUPPORTED: for want of a device)
+        k = size / most_of(shape)
+        coefficients = tuple(k * x for x in shape)
+        assert (most_of(coefficients) < 1024) == (code == EUNSUPPORTED)
+        assert call(host, coefficients=coefficients, steps=1) == code, coefficients
