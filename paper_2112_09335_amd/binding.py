@@ -123,6 +123,30 @@ def _ptr_array(arrs):
     return out
 
 
+def _rows_meet(p, q):
+    """Whether two sets of rows share a byte.  A set: (address, rows, bytes from one row to the next, bytes of a row); its own rows
+    are apart."""
+    (a, n, step, width), (b, m, other, wide) = p, q
+    if n == 0 or m == 0 or a + (n - 1) * step + width <= b or b + (m - 1) * other + wide <= a:
+        return False
+    if n == 1 or step == width:                               # one stretch: the other's first row that ends behind its beginning
+        end, j = a + (n - 1) * step + width, max(0, (a - wide - b) // max(other, 1) + 1) if m > 1 else 0
+        return j < m and b + j * other < end
+    if m == 1 or other == wide:
+        return _rows_meet(q, p)
+    if step == other:                                         # row j of q lies at b - a + (j - i) step from row i of p
+        k = max((a - b - wide) // step + 1, 1 - n)
+        return k < m and b - a + k * step < width
+    if n > m:
+        return _rows_meet(q, p)
+    for i in range(0, n, 1 << 20):                            # every row of p against q's first row that ends behind its beginning
+        at = a + step * np.arange(i, min(i + (1 << 20), n), dtype=np.int64)
+        j = np.maximum((at - wide - b) // other + 1, 0)
+        if ((j < m) & (b + j * other < at + width)).any():
+            return True
+    return False
+
+
 class Solver:
     """One problem instance on one GPU.  Method names mirror the C entry points."""
 
@@ -448,6 +472,21 @@ class Solver:
             return step if inner == 1 or width == 1 else None
         return width if n == 0 or width == 1 or t.stride(1) == 1 else None
 
+    def _apart(self, what, out, step, *operands):
+        """A given output shares no element with what the call reads (rows that interleave do not).  operands: (name, tensor, elements from
+        one row to the next); of a dense tensor the step is None."""
+        def rows(name, t, step):
+            size = t.element_size()
+            if step is None or t.numel() == 0:
+                return t.data_ptr(), min(t.numel(), 1), t.numel() * size, t.numel() * size
+            if step < t.shape[1]:
+                raise CadmmError(f"{what}: rows of {name} overlap each other")
+            return t.data_ptr(), t.shape[0], step * size, t.shape[1] * size
+        own = rows("out", out, step)
+        for operand in operands:
+            if _rows_meet(own, rows(*operand)):
+                raise CadmmError(f"{what}: out overlaps {operand[0]}")
+
     def _scratch(self, query, *args):
         """Scratch of one call, from torch's allocator for the current stream: (aligned pointer, bytes, what keeps it alive)."""
         nbytes = C.c_size_t()
@@ -460,8 +499,9 @@ class Solver:
     def op_transform_grouped(self, A, B, group_ptr, transposed=False, out=None):
         """out[r] = A[r] B_g for the rows r in [group_ptr[g], group_ptr[g + 1]) of every group.  A: n x K, B: groups x K x C
         (transposed: groups x C x K, and B_g is its transpose), group_ptr: int64 device tensor of groups + 1 bounds that do not
-        descend.  `out` may be a preallocated n x C matrix with dense rows: rows of no group are left as they are there, and
-        hold anything otherwise.  With the communities' weights in B: group_ptr = comm_row_ptr of get_graph."""
+        descend.  `out` may be a preallocated n x C matrix with dense rows that shares no element with A, B or group_ptr (it may be other columns of
+        A's buffer): rows of no group are left as they are there, and hold anything otherwise.  With the communities' weights in
+        B: group_ptr = comm_row_ptr of get_graph.  An entry that is not finite leaves NaN or infinities where it enters."""
         torch, types, gpu = self._torch, self._types or self._value_types(), self.device
         dtype = A.dtype
         if A.dim() != 2 or B.dim() != 3 or group_ptr.dim() != 1 or group_ptr.shape[0] < 2:
@@ -469,7 +509,7 @@ class Solver:
         (n, K), (groups, rows, cols) = A.shape, B.shape
         if transposed:
             rows, cols = cols, rows
-        lda = self._row_stride(A)
+        lda, given = self._row_stride(A), out is not None
         fits = (dtype in types and K >= 1 and lda is not None and A.get_device() == gpu and B.get_device() == gpu and B.dtype == dtype and rows == K and
                 B.is_contiguous() and group_ptr.get_device() == gpu and group_ptr.dtype == torch.int64 and
                 group_ptr.shape[0] == groups + 1 and group_ptr.is_contiguous())
@@ -484,6 +524,8 @@ class Solver:
             groups = group_ptr.shape[0] - 1
             self._refuse("op_transform_grouped", types, [("A", A, None, None)] + ([] if out is None else [("out", out, (n, cols), dtype)]),
                          [("group_ptr", group_ptr, (groups + 1,), (torch.int64,)), ("B", B, (groups, cols, K) if transposed else (groups, K, cols), (dtype,))])
+        if given:
+            self._apart("op_transform_grouped", out, ldo, ("A", A, lda), ("B", B, None), ("group_ptr", group_ptr, None))
         self._on_raw_stream()
         rc = self.lib.cadmm_op_transform_grouped(self.h, types[dtype], A.data_ptr(), n, lda, K, B.data_ptr(), cols, 1 if transposed else 0, groups,
                                                  group_ptr.data_ptr(), out.data_ptr(), ldo)
@@ -493,13 +535,14 @@ class Solver:
 
     def op_wgrad_grouped(self, A, G, group_ptr, out=None, out_dtype=None):
         """out[g] = A_g^T G_g over the rows of every group (groups x K x C): the gradient of op_transform_grouped with respect to
-        B.  In fp32 unless `out` or out_dtype (fp32 or the operands' type) says otherwise; zeros for a group without rows."""
+        B.  In fp32 unless `out` (which shares no element with A, G or group_ptr) or out_dtype (fp32 or the operands' type) says
+        otherwise; zeros for a group without rows.  An entry that is not finite leaves NaN or infinities where it enters."""
         torch, types, gpu = self._torch, self._types or self._value_types(), self.device
         dtype = A.dtype
         if A.dim() != 2 or G.dim() != 2 or group_ptr.dim() != 1 or group_ptr.shape[0] < 2:
             raise CadmmError("op_wgrad_grouped: A and G are matrices, group_ptr holds groups + 1 bounds")
         (n, K), (m, width), groups = A.shape, G.shape, group_ptr.shape[0] - 1
-        lda, ldg = self._row_stride(A), self._row_stride(G)
+        lda, ldg, given = self._row_stride(A), self._row_stride(G), out is not None
         wanted = (torch.float32, dtype) if out_dtype is None else (out_dtype,)
         fits = (dtype in types and G.dtype == dtype and m == n and K >= 1 and width >= 1 and lda is not None and ldg is not None and
                 A.get_device() == gpu and G.get_device() == gpu and group_ptr.get_device() == gpu and group_ptr.dtype == torch.int64 and
@@ -511,6 +554,8 @@ class Solver:
         if not fits:
             self._refuse("op_wgrad_grouped", types, [("A", A, None, None), ("G", G, (n, width), dtype)],
                          [("group_ptr", group_ptr, (groups + 1,), (torch.int64,))] + ([] if out is None else [("out", out, (groups, K, width), wanted)]))
+        if given:
+            self._apart("op_wgrad_grouped", out, None, ("A", A, lda), ("G", G, ldg), ("group_ptr", group_ptr, None))
         ptr, nbytes, hold = self._scratch(self.lib.cadmm_op_wgrad_grouped_scratch, n, K, width, groups)
         self._on_raw_stream()
         rc = self.lib.cadmm_op_wgrad_grouped(self.h, types[dtype], A.data_ptr(), n, lda, K, G.data_ptr(), ldg, width, groups,

@@ -366,6 +366,41 @@ def test_refusals_of_tensors(solver):
             solver.op_wgrad_grouped(a, g, p, **more)
 
 
+def test_an_output_that_shares_elements_with_an_operand_is_refused(solver):
+    """Its tiles would be written while others still read them.  Other columns of one buffer, and neighbours in memory, are apart."""
+    import torch
+    from paper_2112_09335_amd.binding import CadmmError
+    n, K = 300, 64
+    rng = np.random.default_rng(52)
+    held = torch.from_numpy(rng.standard_normal((n + 70, 2 * K)).astype(np.float32)).cuda()
+    before = held.clone()
+    ptr = torch.tensor([0, 100, n], device="cuda")
+    B = torch.randn(2, K, K, device="cuda")
+    A = held[:n, :K]
+    flat = held.view(-1)
+    bad = [A, held[:n, 1:K + 1], held[:n, K - 1:2 * K - 1], held[1:n + 1, :K], held[40:n + 40, :K], flat[K:K + n * K].view(n, K),
+           flat[:n * (K + 3)].view(n, K + 3)[:, :K], held[:1, :K].expand(n, K)]
+    for out in bad:
+        with pytest.raises(CadmmError):
+            solver.op_transform_grouped(A, B, ptr, out=out)
+    few = torch.tensor([0, 1, 2], device="cuda")
+    with pytest.raises(CadmmError):
+        solver.op_transform_grouped(A[:2], B, few, out=B[1, 5:7])
+    with pytest.raises(CadmmError):
+        solver.op_transform_grouped(A[:2, :3].contiguous(), B[:, :3, :3].contiguous(), few, out=few.view(torch.float32)[:6].view(2, 3))
+    for out in (flat[:2 * K * K].view(2, K, K), flat[2 * K * (n - 1):2 * K * (n - 1) + 2 * K * K].view(2, K, K)):
+        with pytest.raises(CadmmError):
+            solver.op_wgrad_grouped(A, A.contiguous(), ptr, out=out)
+        with pytest.raises(CadmmError):
+            solver.op_wgrad_grouped(A.contiguous(), A, ptr, out=out)
+    assert torch.equal(held, before)
+    want = solver.op_transform_grouped(A, B, ptr)
+    assert torch.equal(solver.op_transform_grouped(A, B, ptr, out=held[:n, K:]), want) and torch.equal(held[:, :K], before[:, :K])
+    dB = solver.op_wgrad_grouped(A, A, ptr)
+    at = flat[2 * K * (n - 1) + K:][:2 * K * K].view(2, K, K)                # right behind A's last row
+    assert torch.equal(solver.op_wgrad_grouped(A, A, ptr, out=at), dB) and torch.equal(held[:n, :K], before[:n, :K])
+
+
 def test_no_rows_at_all(solver):
     import torch
     ptr = torch.zeros(4, dtype=torch.int64, device="cuda")

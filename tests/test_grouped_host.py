@@ -172,3 +172,23 @@ def test_growth_is_judged_by_the_largest_value_wherever_it_lies(host, call, shap
         coefficients = tuple(k * x for x in shape)
         assert (most_of(coefficients) < 1024) == (code == EUNSUPPORTED)
         assert call(host, coefficients=coefficients, steps=1) == code, coefficients
+
+
+def test_sets_of_rows_meet_where_they_share_a_byte():
+    rng = np.random.default_rng(1)
+    seen = [0, 0]
+    for _ in range(20000):
+        sets = []
+        for _ in range(2):
+            width = int(rng.integers(1, 6))
+            sets.append((int(rng.integers(0, 40)), int(rng.integers(0, 7)), width + int(rng.choice([0, 0, 1, 3, 7, 11])), width))
+        if rng.random() < 0.5:
+            sets[1] = (sets[1][0], sets[1][1], max(sets[0][2], sets[1][3]), sets[1][3])      # rows equally far apart
+        bytes_of = [{at + i * step + k for i in range(n) for k in range(width)} for at, n, step, width in sets]
+        meet = bool(bytes_of[0] & bytes_of[1])
+        assert binding._rows_meet(*sets) == meet and binding._rows_meet(*sets[::-1]) == meet, sets
+        seen[meet] += 1
+    assert min(seen) > 2000
+    far = (1 << 46, 3 << 20, 100, 40)
+    assert not binding._rows_meet(far, ((1 << 46) + 40, 3 << 20, 100, 60)) and binding._rows_meet(far, ((1 << 46) + 39, 3 << 20, 100, 60))
+    assert binding._rows_meet(far, ((1 << 46) + 40, 3 << 20, 101, 60)) and not binding._rows_meet(far, ((1 << 46) + 40, 3 << 20, 200, 60))
