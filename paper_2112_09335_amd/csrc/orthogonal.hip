@@ -300,7 +300,7 @@ __global__ __launch_bounds__(1024) void orthogonal_block_kernel(Source<T> src, c
                                                                 float scale, int slabs, int one, int step, int steps, Schedule sch,
                                                                 char* __restrict__ images, const float* __restrict__ parts_in, int n_parts,
                                                                 float* __restrict__ parts_out,
-                                                                T* __restrict__ out, float* __restrict__ W, float keep, float rate) {
+                                                                T* out, float* W, float keep, float rate) {       // (out may be src.G)
     constexpr int R = 32 * RT, WIDTH = kBlockX / 4 / R, CT = WIDTH / 32;         // rows, columns of the slab, tiles of 32 columns
     constexpr int GROUPS = 16 / (RT * RT);                                   // wavefronts that share a tile of S
     using XRows = Rows<WIDTH / 4>;

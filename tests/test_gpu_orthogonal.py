@@ -205,6 +205,15 @@ def test_into_its_own_input_and_from_any_element(solver):
         assert torch.equal(solver.op_orthogonalise(at, out=at), want)
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("batch,K,width", [(1, 256, 64), (3, 64, 200), (40, 12, 20), (2, 128, 128), (3, 128, 300), (2, 700, 33), (1, 260, 130), (7, 140, 520)])
+def test_into_its_own_input_whichever_way_it_is_computed(solver, kind, batch, K, width):
+    import torch
+    G = gradient(torch, 29, batch, K, width, kind).cuda()
+    want = solver.op_orthogonalise(G)
+    assert solver.op_orthogonalise(G, out=G) is G and torch.equal(G, want)
+
+
 def test_streams_and_captured_graphs(solver):
     """Two captured graphs and eager calls, each with scratch of its own, replayed in turn."""
     import torch
