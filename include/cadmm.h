@@ -250,7 +250,8 @@ int  cadmm_op_wgrad_noalloc(cadmm_ctx* ctx, const float* A, const float* G, int6
  * No atomics: the same call gives the same bits.  n = 0 is allowed (A, G and transform_grouped's out may then be null).
  * wgrad_grouped needs device scratch of _scratch bytes, 256-byte aligned, that no other call uses until it is done; nothing in
  * it has to be cleared.  Neither call needs a graph, model or workspace.  Both run on the stream of the kernel-level calls and make the
- * context's device current for themselves.  At most 65536 columns, 2^20 groups, and result tiles for 2^22 workgroups (CADMM_EUNSUPPORTED beyond).
+ * context's device current for themselves.  At most 65536 columns, 2^20 groups and 2^40 rows (CADMM_EINVAL beyond), and result tiles for
+ * 2^22 workgroups (CADMM_EUNSUPPORTED beyond).
  */
 #define CADMM_F32  0
 #define CADMM_BF16 1

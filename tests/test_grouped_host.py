@@ -1,5 +1,6 @@
 """Refusals of the products over groups of rows and of the orthogonalised updates, and the streams and devices they use: no GPU call."""
 import ctypes as C
+import os
 
 import numpy as np
 import pytest
@@ -192,3 +193,19 @@ def test_sets_of_rows_meet_where_they_share_a_byte():
     far = (1 << 46, 3 << 20, 100, 40)
     assert not binding._rows_meet(far, ((1 << 46) + 40, 3 << 20, 100, 60)) and binding._rows_meet(far, ((1 << 46) + 39, 3 << 20, 100, 60))
     assert binding._rows_meet(far, ((1 << 46) + 40, 3 << 20, 101, 60)) and not binding._rows_meet(far, ((1 << 46) + 40, 3 << 20, 200, 60))
+
+
+def test_sizes_past_the_limits_give_the_codes_that_the_header_names(host):
+    need = C.c_size_t()
+    query = host.lib.cadmm_op_wgrad_grouped_scratch
+    most = dict(n=1 << 40, K=1 << 16, width=1 << 16, groups=1 << 20)
+    for size, stride in dict(n=None, K="lda", width="ldo", groups=None).items():
+        past = most[size] + 1
+        assert transform(host, **{size: past}, **({stride: past} if stride else {})) == EINVAL
+        assert wgrad(host, **{size: past}, **({"ldg" if stride == "ldo" else stride: past} if stride else {})) == EINVAL
+        sizes = {**dict(n=10, K=8, width=4, groups=2), size: past}
+        assert query(host.h, sizes["n"], sizes["K"], sizes["width"], sizes["groups"], C.byref(need)) == EINVAL
+        sizes[size] = most[size]
+        assert query(host.h, sizes["n"], sizes["K"], sizes["width"], sizes["groups"], C.byref(need)) == OK
+    text = " ".join(open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "cadmm.h")).read().replace(" * ", " ").split())
+    assert "At most 65536 columns, 2^20 groups and 2^40 rows (CADMM_EINVAL beyond), and result tiles for 2^22 workgroups (CADMM_EUNSUPPORTED beyond)" in text
