@@ -275,7 +275,7 @@ int  cadmm_op_wgrad_grouped(cadmm_ctx* ctx, int32_t type, const void* A, int64_t
  *                   out may be G itself, and overlaps it in no other way.
  *   muon_step:      M <- momentum M + G;  D = G + momentum M with nesterov, else M;  W <- (1 - lr weight_decay) W - lr scale O with
  *                   O the orthogonalised D.  W, M: device batch x K x C, fp32, updated in place; G of `type`, not changed.  The three
- *                   do not overlap.
+ *                   do not overlap.  1 - lr weight_decay and lr scale are finite in fp32 (CADMM_EINVAL).
  * 1 <= steps <= 64; eps >= 0; coefficients under which a singular value in [0, 1] could grow past 1024 on the way are CADMM_EINVAL.  Products take
  * their operands with 22 bits (pairs of fp16) and are summed in fp32, norms in fp64.  No atomics: the same call gives the
  * same bits.  scratch: device, _scratch bytes, 256-byte aligned, used by no other call until this one is done; nothing in it has to be

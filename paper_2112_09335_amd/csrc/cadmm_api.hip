@@ -2021,6 +2021,7 @@ int cadmm_op_muon_step(cadmm_ctx* c, int32_t type, const void* G, float* W, floa
     a.G = G; a.batch = batch; a.K = K; a.C = C; a.steps = steps; a.eps = eps; a.scratch = scratch;
     a.W = W; a.M = M; a.mu = momentum; a.nesterov = nesterov != 0;
     a.keep = (float)(1.0 - (double)lr * weight_decay); a.rate = (float)((double)lr * scale);
+    if (!std::isfinite(a.keep) || !std::isfinite(a.rate)) return fail(c, CADMM_EINVAL, "lr weight_decay and lr scale must be finite in fp32");
     return orthogonalise(c, "op_muon_step", type, a, coefficients, scratch_bytes);
 }
 

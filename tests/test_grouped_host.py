@@ -209,3 +209,10 @@ def test_sizes_past_the_limits_give_the_codes_that_the_header_names(host):
         assert query(host.h, sizes["n"], sizes["K"], sizes["width"], sizes["groups"], C.byref(need)) == OK
     text = " ".join(open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "cadmm.h")).read().replace(" * ", " ").split())
     assert "At most 65536 columns, 2^20 groups and 2^40 rows (CADMM_EINVAL beyond), and result tiles for 2^22 workgroups (CADMM_EUNSUPPORTED beyond)" in text
+
+
+@pytest.mark.parametrize("wrong", [dict(lr=1e30, scale=1e30), dict(lr=-1e30, scale=1e30), dict(lr=1e30, decay=1e30), dict(lr=3e38, scale=1.2)])
+def test_rates_past_the_largest_number_are_refused(host, wrong):
+    """Infinite in fp32, they would make NaN of every weight whose update is zero."""
+    assert muon(host, **wrong) == EINVAL
+    assert muon(host, **{**wrong, "lr": 1e-30}) == EUNSUPPORTED                # (for want of a device)
