@@ -592,8 +592,11 @@ struct Direct : Tile<WM_, WN_, TM_, TN_, WK_> {
 };
 
 // One quad of a row of `width` results at column c (c < width), the row at `to`; whole: width and the row's place are multiples of four
-// elements.  STREAM: past the caches' order of use, for results that are larger than what the tiles read (16384 x 2048 x 1024 in 64 groups,
-// 537 MB of them: 212 -> 200 us).
+// elements.  STREAM: past the caches' order of use, as all weight gradients over groups that are not summed in parts are stored.  With plain
+// stores for it: results of up to 17 MB take the same 15 us; 67 MB 24.5 us for 26.0 (4096 x 1024 x 1024 bf16 to fp32, 16 groups), 134 MB 54.5 for
+// 64.3 (16384 rows, 32 groups), 537 MB 164 for 173 (16384 x 2048 x 1024, 64 even groups).  A call behind it that reads the result finds less of it
+// in the caches: with an optimiser step the two take 403 us for 398, 783 for 777 (the first two above), 1347 for 1367 (268 MB); what loses most is
+// a result that is nearly the whole work and is read in one pass (200 rows in 64 groups of 1024 x 1024, 268 MB: 155 for 133).
 template <bool STREAM = false, class O>
 __device__ __forceinline__ void put(O* to, int c, int width, float4 v, bool whole) {
     typedef O ox4 __attribute__((ext_vector_type(4)));
