@@ -5,7 +5,7 @@
 // them (an element's k is its row: kAcross), and is one of
 //   bf16 / fp16   as they are, one product per pair of elements;
 //   Pair          two fp16 whose sum is the value, 22 bits of significand: three products (the fourth is below 2^-22); eight high
-//                 parts are followed by their eight low ones in memory;
+//                 parts are followed by their eight low ones in memory (straight to LDS only: Direct, below);
 //   float         split on the way into three bf16 parts, exactly (8 + 8 + 8 bits): six products (the other three are below 2^-24).
 //
 // Way of the data: chunks of eight k (kAlong) or eight i (kAcross) from memory into registers, PF steps of BK ahead; from there,
@@ -55,7 +55,6 @@ template <> inline constexpr int kParts<float> = 3;
 
 // a chunk of eight elements as loaded
 template <class T> struct Chunk { uintx4 v[1]; };
-template <> struct Chunk<Pair> { uintx4 v[2]; };
 template <> struct Chunk<float> { uintx4 v[2]; };
 
 typedef unsigned uintx4a4 __attribute__((ext_vector_type(4), aligned(4)));
@@ -222,7 +221,6 @@ struct Operand {
                 to[2 * (kPlane / 8)] = uintx4{l[0], l[1], l[2], l[3]};
             } else {
                 to[0] = v.v[0];
-                if constexpr (kParts_ == 2) to[kPlane / 8] = v.v[1];
             }
         }
     }
@@ -349,11 +347,12 @@ struct Tile {
     __device__ __forceinline__ static void drain(floatx16 (&acc)[TM][TN], unsigned short* S, F f) { drain<false>(acc, S, f, [](int, int, float4) {}); }
 };
 
-// Tiles whose operands go through registers: any operand, any rows.
+// Tiles whose operands go through registers: fp32, bf16 or fp16, any rows.
 template <class T, Lie XL, Lie YL, Mode MODE, int WM_, int WN_, int TM_, int TN_, int BK_, int PF_, int BUFFERS_, int WK_ = 1>
 struct Product : Tile<WM_, WN_, TM_, TN_, WK_> {
     using Base = Tile<WM_, WN_, TM_, TN_, WK_>;
     using Base::WM; using Base::WN; using Base::TM; using Base::TN; using Base::WK; using Base::BM; using Base::BN; using Base::THREADS; using Base::kSlabs;
+    static_assert(kParts<T> != 2, "Pairs go straight to LDS");
     static constexpr int BK = BK_, PF = PF_, BUFFERS = BUFFERS_;
     using X = Operand<T, XL, MODE, BM, BK, 64 * WM * WN, PF, WK>;
     using Y = Operand<T, YL, MODE, BN, BK, 64 * WM * WN, PF, WK>;
@@ -380,8 +379,7 @@ struct Product : Tile<WM_, WN_, TM_, TN_, WK_> {
                     for (int i = 0; i < TM; ++i) acc[i][j] = multiply<T>(b[p], a[q][i], acc[i][j]);
                 };
                 // smallest terms first
-                if constexpr (P == 3) { add(0, 2); add(2, 0); add(1, 1); }
-                if constexpr (P >= 2) { add(0, 1); add(1, 0); }
+                if constexpr (P == 3) { add(0, 2); add(2, 0); add(1, 1); add(0, 1); add(1, 0); }
                 add(0, 0);
             }
         }
