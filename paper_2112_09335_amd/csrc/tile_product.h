@@ -6,7 +6,7 @@
 //   bf16 / fp16   as they are, one product per pair of elements;
 //   Pair          two fp16 whose sum is the value, 22 bits of significand: three products (the fourth is below 2^-22); eight high
 //                 parts are followed by their eight low ones in memory (straight to LDS only: Direct, below);
-//   float         split on the way into three bf16 parts, exactly (8 + 8 + 8 bits): six products (the other three are below 2^-24).
+//   float         split on the way into three bf16 parts, exactly (8 + 8 + 8 bits): six products (the other three are below 2^-24 together).
 //
 // Way of the data: chunks of eight k (kAlong) or eight i (kAcross) from memory into registers, PF steps of BK ahead; from there,
 // split where need be, to LDS; from there into the matrix cores' operand layout, eight k of one row per lane.  With two LDS
@@ -122,14 +122,19 @@ __device__ __forceinline__ void settle(Chunk<T>& q, int c, int width, bool in) {
     __builtin_memcpy(&q, w, sizeof(q));
 }
 
-// two fp32 numbers -> their three bf16 parts, each pair packed into one dword (low half = first number)
+// Two fp32 numbers -> their three bf16 parts, each pair packed into one dword (low half = first number).  The first two are the nearest
+// bf16 numbers, so that a part is at most 2^-8 of what it is the rest of; the last is what is left, 8 bits at most.  (Truncated, parts are up to 2^-7 of it
+// and of one sign: the products that are left out would add up to 2^-21, always towards zero.)  Numbers that would round to infinity
+// get the largest bf16 number.
 __device__ __forceinline__ void three_parts(float x0, float x1, unsigned& h, unsigned& m, unsigned& l) {
-    const unsigned u0 = __float_as_uint(x0), u1 = __float_as_uint(x1);
-    h = __builtin_amdgcn_perm(u1, u0, 0x07060302u);                     // upper halves of u1 and u0
-    const float r0 = x0 - __uint_as_float(u0 & 0xFFFF0000u), r1 = x1 - __uint_as_float(u1 & 0xFFFF0000u);          // exact
-    const unsigned v0 = __float_as_uint(r0), v1 = __float_as_uint(r1);
-    m = __builtin_amdgcn_perm(v1, v0, 0x07060302u);
-    const float s0 = r0 - __uint_as_float(v0 & 0xFFFF0000u), s1 = r1 - __uint_as_float(v1 & 0xFFFF0000u);          // exact, 8 bits at most
+    typedef float floatx2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    auto nearest = [](float a, float b) { return __builtin_bit_cast(unsigned, __builtin_convertvector((floatx2{a, b}), bf16x2)); };
+    const float most = __uint_as_float(0x7F7F0000u);
+    h = nearest(__builtin_amdgcn_fmed3f(x0, -most, most), __builtin_amdgcn_fmed3f(x1, -most, most));
+    const float r0 = x0 - __uint_as_float(h << 16), r1 = x1 - __uint_as_float(h & 0xFFFF0000u);              // exact
+    m = nearest(r0, r1);
+    const float s0 = r0 - __uint_as_float(m << 16), s1 = r1 - __uint_as_float(m & 0xFFFF0000u);              // exact
     l = __builtin_amdgcn_perm(__float_as_uint(s1), __float_as_uint(s0), 0x07060302u);
 }
 

@@ -401,6 +401,30 @@ def test_an_output_that_shares_elements_with_an_operand_is_refused(solver):
     assert torch.equal(solver.op_wgrad_grouped(A, A, ptr, out=at), dB) and torch.equal(held[:n, :K], before[:n, :K])
 
 
+@pytest.mark.parametrize("rows", [300, 40, 7])
+def test_every_product_of_two_fp32_numbers(solver, rows):
+    """Sums of one product: the three parts leave out less than 2^-24 (1 + 2^-8) of it, an instruction may be off by a step (2^-23) in adding
+    the largest terms, and in adding those below 2^-7 of them by 2^-30 each: less than 4 * 2^-24 in all.  Numbers whose bits behind the eighth
+    are all ones or just beyond a tie, random ones, and the largest of all against small ones."""
+    import torch
+    rng = np.random.default_rng(53)
+    bits = np.array([0x3f80ffff, 0x3f807fff, 0x3f808001, 0x3f817f80, 0x3f80ff80, 0x3fffffff, 0x3f800000, 0x3f80807f, 0x3fc07f7f, 0x3f810001], np.uint32)
+    x = np.concatenate([bits.view(np.float32), rng.uniform(1.0, 2.0, 290).astype(np.float32)])
+    x *= np.exp2(rng.integers(-60, 60, 300)).astype(np.float32) * rng.choice([-1, 1], 300).astype(np.float32)
+    y = rng.permutation(x)[:200] * np.float32(2.0 ** -3)
+    largest = np.array([0x7f7fffff, 0x7f7f8000, 0x7f7f7fff, 0x7f7f8001, 0xff7fffff], np.uint32).view(np.float32)
+    for a, b in ((x[:rows], y), (largest, np.concatenate([bits[:7].view(np.float32) * np.float32(2.0 ** -k) for k in (1, 40, 100)]))):
+        want = np.outer(a.astype(np.float64), b.astype(np.float64))
+        A, B = torch.from_numpy(a).view(-1, 1), torch.from_numpy(b)
+        ptr = torch.tensor([0, len(a)])
+        got = [solver.op_transform_grouped(A.cuda(), B.view(1, 1, -1).cuda(), ptr.cuda()),
+               solver.op_transform_grouped(A.cuda(), B.view(1, -1, 1).cuda(), ptr.cuda(), transposed=True),
+               solver.op_wgrad_grouped(A.view(1, -1).cuda(), B.view(1, -1).cuda(), torch.tensor([0, 1]).cuda())[0]]
+        for g in got:
+            far = np.abs(g.cpu().double().numpy() - want) / np.abs(want)
+            assert far.max() < 4 * 2.0 ** -24, (far.max() * 2.0 ** 24, np.unravel_index(far.argmax(), far.shape))
+
+
 def test_no_rows_at_all(solver):
     import torch
     ptr = torch.zeros(4, dtype=torch.int64, device="cuda")
