@@ -114,6 +114,15 @@ def test_product_over_groups_that_fills_the_chip(solver, kind, transposed, sizes
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("sizes,K,width", [([4000, 9000, 0, 1, 5010, 8000, 4000], 97, 301), ([25000, 15000], 136, 128), ([40] * 70, 264, 200), ([40] * 70, 261, 201),
+                                           ([2] * 64, 264, 640), ([2] * 64, 261, 645)], ids=lambda v: str(v).replace(" ", "")[:24])
+def test_product_over_groups_in_every_size_of_tiles(solver, kind, transposed, sizes, K, width):
+    """As above: 128 x 128 with unaligned rows and with few columns, 64 x 64 and 32 x 64 without sets that share the contraction."""
+    test_product_over_groups_that_fills_the_chip(solver, kind, transposed, sizes, K, width)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("sizes,K,width", [([30000, 0, 41000, 7], 264, 392), ([60000], 520, 520), ([40000, 20001], 301, 200), ([700] * 40, 1024, 1032)],
                          ids=lambda v: str(v).replace(" ", "")[:24])
 def test_weight_gradient_over_groups_that_fills_the_chip(solver, kind, sizes, K, width):
@@ -129,6 +138,13 @@ def test_weight_gradient_over_groups_that_fills_the_chip(solver, kind, sizes, K,
     out = solver.op_wgrad_grouped(A.cuda(), G.cuda(), ptr.cuda())
     close(out, want.cpu().numpy(), size.cpu().numpy(), max(sizes), "f32")
     assert torch.equal(out, solver.op_wgrad_grouped(A.cuda(), G.cuda(), ptr.cuda()))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("sizes,K,width", [([25000] * 8, 64, 64), ([60000], 521, 523)], ids=lambda v: str(v).replace(" ", "")[:24])
+def test_weight_gradient_over_groups_in_every_size_of_tiles(solver, kind, sizes, K, width):
+    """As above: 64 x 64 without sets that share the contraction, 128 x 256 with unaligned rows."""
+    test_weight_gradient_over_groups_that_fills_the_chip(solver, kind, sizes, K, width)
 
 
 @pytest.mark.parametrize("kind,out_kind", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16"), ("f16", "f32"), ("f16", "f16")])
@@ -234,6 +250,43 @@ def test_bounds_past_the_rows_are_clamped(solver):
         assert (held[0] == 3.0).all() and (held[201] == 3.0).all()
         dB = solver.op_wgrad_grouped(A.cuda(), A.cuda(), torch.tensor(ptr).cuda())
         close(dB, *want_tn(A, A, torch.tensor([0, 60, 200, 200])), 200, "f32")
+
+
+@pytest.mark.parametrize("kind,K,width,n", [("f32", 64, 64, 5000), ("bf16", 256, 256, 5000), ("f32", 33, 70, 3000), ("bf16", 300, 24, 90)])
+def test_descending_bounds_touch_nothing_outside(solver, kind, K, width, n):
+    """What the rows and matrices hold is not specified then; the rows around out and what lies around the gradient and its scratch stay as they
+    are, as do the operands."""
+    import ctypes as C
+    import torch
+    t = types()[kind]
+    rng = np.random.default_rng(54)
+    A, D = torch.randn(n, K, device="cuda").to(t), torch.randn(n, width, device="cuda").to(t)
+    lib, h = solver.lib, solver.h
+    for trial in range(6):
+        groups = (1, 2, 7, 64, 65, 300)[trial]
+        bounds = rng.integers(-n, 2 * n, groups + 1)
+        bounds[0], bounds[-1] = (n, 0) if trial % 2 else (bounds[0], bounds[-1])
+        ptr = torch.from_numpy(np.sort(bounds)[::-1].copy() if trial < 2 else bounds).cuda()
+        B = torch.randn(groups, K, width, device="cuda").to(t)
+        A0, B0, D0 = A.clone(), B.clone(), D.clone()
+        held = torch.full((n + 300, width), 7.0, dtype=t, device="cuda")
+        solver.op_transform_grouped(A, B, ptr, out=held[150:150 + n])
+        need = C.c_size_t()
+        assert lib.cadmm_op_wgrad_grouped_scratch(h, n, K, width, groups, C.byref(need)) == 0
+        around = 1 << 20
+        scratch = torch.full((need.value + 2 * around,), 77, dtype=torch.uint8, device="cuda")
+        at = (scratch.data_ptr() + around + 255) & ~255
+        dB = torch.full((groups * K * width + 20000,), 7.0, device="cuda")
+        solver._on_raw_stream()
+        rc = lib.cadmm_op_wgrad_grouped(h, {"f32": 0, "bf16": 1}[kind], A.data_ptr(), n, K, K, D.data_ptr(), width, width, groups, ptr.data_ptr(), 0,
+                                        dB.data_ptr() + 40000, at, need.value)
+        assert rc == 0
+        torch.cuda.synchronize()
+        first = at - scratch.data_ptr()
+        assert (held[:150] == 7).all() and (held[150 + n:] == 7).all()
+        assert (dB[:10000] == 7).all() and (dB[10000 + groups * K * width:] == 7).all()
+        assert (scratch[:first] == 77).all() and (scratch[first + need.value:] == 77).all()
+        assert torch.equal(A, A0) and torch.equal(B, B0) and torch.equal(D, D0)
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32"])

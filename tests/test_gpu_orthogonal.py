@@ -93,6 +93,17 @@ def test_stacks_that_fill_the_chip(solver, kind, times, K, width):
     check(out[0].cpu(), G, kind)
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("times,K,width", [(76, 514, 520), (76, 520, 514), (10, 300, 513), (10, 513, 300), (3, 513, 300), (3, 512, 513)])
+def test_stacks_of_every_size_of_tiles(solver, kind, times, K, width):
+    """As above, at the sizes where tiles of 256 x 256 of the symmetric products, 128 x 128 and 64 x 64 of the others are taken, wide and tall."""
+    test_stacks_that_fill_the_chip(solver, kind, times, K, width)
+
+
+def test_optimiser_step_of_the_hidden_layers_of_a_deep_model(solver):
+    test_optimiser_step(solver, "f32", True, 7, 512, 512)
+
+
 @pytest.mark.parametrize("coefficients,steps", [(MUON, 1), (MUON, 2), (MUON, 10), ((1.5, -0.5, 0.0), 12), ((15 / 8, -10 / 8, 3 / 8), 8), ((4.0, 0.0, 0.0), 4),
                                                 ((0.0, 1.0, 0.0), 1), ((-2.0, 0.5, 0.25), 3), ((0.5, 0.0, 0.0), 3)])
 @pytest.mark.parametrize("batch,K,width", [(2, 48, 80), (1, 260, 130), (1, 128, 512)])
