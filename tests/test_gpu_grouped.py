@@ -147,6 +147,17 @@ def test_weight_gradient_over_groups_in_every_size_of_tiles(solver, kind, sizes,
     test_weight_gradient_over_groups_that_fills_the_chip(solver, kind, sizes, K, width)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("sizes,K,width", [([25000] * 8, 64, 64), ([60000], 521, 523), ([30000, 0, 41000, 7], 264, 392), ([700] * 40, 1024, 1032), ([40000, 20001], 301, 200)],
+                         ids=lambda v: str(v).replace(" ", "")[:24])
+def test_weight_gradient_of_16_bits_is_the_rounded_one(solver, kind, sizes, K, width):
+    """The sums are the same (tested against 64 bits above), rounded once at the end."""
+    import torch
+    A, _, ptr = (x.cuda() for x in draw(torch, K, sizes, K, 1, kind))
+    G = draw(torch, K + 1, sizes, width, 1, kind, scale=2.0 ** -5)[0].cuda()
+    assert torch.equal(solver.op_wgrad_grouped(A, G, ptr, out_dtype=types()[kind]), solver.op_wgrad_grouped(A, G, ptr).to(types()[kind]))
+
+
 @pytest.mark.parametrize("kind,out_kind", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16"), ("f16", "f32"), ("f16", "f16")])
 @pytest.mark.parametrize("sizes,K,width", SHAPES + [([20000, 3, 9000], 64, 48), ([70000], 24, 5), ([4096, 4097], 256, 256), ([40000], 130, 130)],
                          ids=lambda v: str(v).replace(" ", "")[:24])

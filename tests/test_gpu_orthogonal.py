@@ -100,6 +100,11 @@ def test_stacks_of_every_size_of_tiles(solver, kind, times, K, width):
     test_stacks_that_fill_the_chip(solver, kind, times, K, width)
 
 
+@pytest.mark.parametrize("times,K,width", [(25, 520, 700), (25, 700, 520), (10, 300, 513), (10, 513, 300), (3, 512, 513), (3, 513, 300)])
+def test_stacks_in_fp16(solver, times, K, width):
+    test_stacks_that_fill_the_chip(solver, "f16", times, K, width)
+
+
 def test_optimiser_step_of_the_hidden_layers_of_a_deep_model(solver):
     test_optimiser_step(solver, "f32", True, 7, 512, 512)
 
