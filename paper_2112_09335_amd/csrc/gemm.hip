@@ -526,7 +526,7 @@ __global__ __launch_bounds__(256) void gemm_nn_narrow_kernel(const float* __rest
 // The same product out[n x C] = A[n x K] B[K x C] on the bf16 matrix cores, fp32-exact in its inputs: an fp32 number is the
 // exact sum of three bf16 numbers (8 + 8 + 8 significand bits, each part the truncated remainder of the one before), and of the
 // nine cross products the six largest are accumulated in fp32 (hi*hi, hi*mid, mid*hi, mid*mid, hi*lo, lo*hi; the three
-// that are left out are below 2^-24 of |a||b|).  Six v_mfma_f32_32x32x16_bf16 per 16 columns of K replace 32
+// that are left out are below 2^-21 of |a||b|, 2^-24 on average).  Six v_mfma_f32_32x32x16_bf16 per 16 columns of K replace 32
 // v_mfma_f32_32x32x2_f32, at a sixteenth of the cycles per flop.  Operand layout of 32x32x16 (64 lanes): a lane holds
 // A[i = lane%32][k = 8*(lane/32) .. +7] and B[k = 8*(lane/32) .. +7][j = lane%32]; the accumulator as for 32x32x2.
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -707,15 +707,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T == 2 ? 4 
 
 // ------------------------------------------------------------------------------------------------ NN, pairs of fp16
 // The same product with half the matrix instructions: an operand scaled by a power of two so that its largest entry lies in
-// [2^14, 2^15) is the sum of two fp16 numbers, x = hi + lo, hi = fp16(x) and lo = fp16(x - hi) rounded to nearest, to 2^-24 of
-// itself or 2^-25, whichever is more, and hi*hi, hi*lo and lo*hi are accumulated in fp32; lo*lo is below 2^-24 of |a||b|.  A row of A
+// [2^14, 2^15) is the sum of two fp16 numbers, x = hi + lo, hi = fp16(x) and lo = fp16(x - hi) rounded to nearest, to 2^-23 of
+// itself or 2^-25, whichever is more, and hi*hi, hi*lo and lo*hi are accumulated in fp32; lo*lo is below 2^-22 of |a||b|.  A row of A
 // has a scale of its own (from RowRange, left by whatever formed A), so has a column of B; results are scaled back by ldexp.
 // Entries far below the largest of their row or column are not held to 24 bits of themselves.  That is of no account where enough
 // of a row's largest entries meet large ones of the column, and a tile of results is formed on pairs only if that is certain for
 // each of them, by counting alone: if of the n entries of a row that are not zero l are near the largest, and of a column s are not
 // near its largest (zeros among them), at least l - s products have two near factors.  Near: at least 2^-6 (2^-7 in a column) of the
 // power of two in the largest, scaled 2^8 and 2^7.  With l - s >= n / 16 the sum |a||b| is at least n / 16 * 2^15, what the 2^-25
-// add up to at most 2 n 2^15 2^-25, and a result is within 3 * 2^-24 + 2^-20 of |a||b|, usually a tenth of that and less.  A tile for
+// add up to at most 2 n 2^15 2^-25, and a result is within 2^-21 + 2^-20 of |a||b|, usually a tenth of that and less.  A tile for
 // which the counts do not say so (features of some columns 1e6 times the others', one-hot weights, rows with few entries) is formed
 // from bf16 triples like the products of gemm_nn_split_kernel, to the bit.
 // What bounds wide products is the power the matrix instructions take (the chip runs them at 1.55 to 1.65 GHz, by GRBM_GUI_ACTIVE over
