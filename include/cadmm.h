@@ -272,7 +272,8 @@ int  cadmm_op_wgrad_grouped(cadmm_ctx* ctx, int32_t type, const void* A, int64_t
  *                   X <- a X + (b S + c S^2) X,  S = X X^T (K <= C; else the same of the transpose), coefficients = host {a, b, c}:
  *                   singular vectors stay, a singular value x becomes a x + b x^3 + c x^5.  out: device, as G.  A zero matrix gives
  *                   zeros (with eps = 0 too), one with an entry that is not finite NaNs throughout; the other matrices are not
- *                   concerned.  Entries of X are held to 2^-36 of one: of a G far below eps, little is left.
+ *                   concerned.  Entries of X are held to 2^-36 of one and 22 bits: of a G far below eps little is left, and a row or column
+ *                   far below the others is less exact than in fp32 (at 1e-4 of them as exact, at 1e-8 off by 5 % of itself).
  *                   out may be G itself, and overlaps it in no other way.
  *   muon_step:      M <- momentum M + G;  D = G + momentum M with nesterov, else M;  W <- (1 - lr weight_decay) W - lr scale O with
  *                   O the orthogonalised D.  W, M: device batch x K x C, fp32, updated in place; G of `type`, not changed.  The three

@@ -146,13 +146,13 @@ void with_type(int type, F f) {
 // LDS, stages, sets of wavefronts and contraction per step.
 //   kLarge  operands are read from LDS once for 128 x 256 results (two workgroups a compute unit) or 256 x 256.  16-bit transform, K = 512,
 //           500000 rows: 128 x 256 391 us, 256 x 256 407, 128 x 128 431 (a library product of one matrix: 389); fp32, through registers,
-//           is faster in 128 x 128 at every size tried (200000 x 256 x 256 165 us for 171) and has no larger ones.  16-bit wgrad:
-//           256 x 256 202 us, 128 x 256 214 (16384 x 2048 x 1024, 64 groups).
+//           is faster in 128 x 128 at every size tried (200000 x 256 x 256 170 us for 179, 20000 x 1024 x 1024 228 for 281) and has no larger
+//           ones.  16-bit wgrad: 256 x 256 202 us, 128 x 256 214 (16384 x 2048 x 1024, 64 ragged groups).
 //   kMiddle 128 x 128;  kSmall 64 x 64, where larger ones would not give every compute unit one
 //   kFew    32 x 64, for groups of a few rows: reading the weights is all there is to it, from many places and far ahead.
 //   kLone.. the same tiles, with more sets of wavefronts to share the contraction, where that leaves no compute unit a second workgroup
-//           anyway.  fp32: one row of 512 x 512 15.9 -> 8.5 us, 16 rows through 16 x 2048 x 1024 71 -> 56, but 64 rows through 64 of them
-//           103 -> 125; 300 x 1000 x 1000 in 4 groups 25.7 -> 22.4, but 100000 x 64 x 64 16.5 -> 28.
+//           anyway.  fp32: one row of 512 x 512 15.7 -> 9.3 us, 16 rows through 16 x 2048 x 1024 57 -> 37, but 64 rows through 64 of them
+//           103 -> 125; 300 x 1000 x 1000 in 4 groups 26.9 -> 24.5, but 100000 x 64 x 64 16.5 -> 28.
 template <class T> constexpr int kStep = 128 / sizeof(T);
 enum Size { kLarge, kMiddle, kSmall, kFew, kLoneSmall, kLoneFew };
 template <class T, Lie X, Lie Y, Mode M, bool STRAIGHT = sizeof(T) == 2 && M == kWhole>
