@@ -245,8 +245,8 @@ int  cadmm_op_wgrad_noalloc(cadmm_ctx* ctx, const float* A, const float* G, int6
  * type: of A, B, G and of out (wgrad_grouped: out_type, the same or CADMM_F32).  lda, ldg, ldo: elements from one row to the next, at least
  * the row's length; B and wgrad_grouped's out are dense.  Pointers need the alignment of their elements only.  Outputs share no element
  * with inputs or scratch, which is the caller's to see to (rows that interleave in one buffer are apart): their tiles are written while others
- * still read.  Products are summed in fp32 and rounded once; fp32 operands count with all 24 bits of their significands, a product
- * being off by less than 2^-24 of itself before it is summed (one within 2^-7 of the largest number may come out infinite).  An operand
+ * still read.  Products are summed in fp32 and rounded once; fp32 operands count with all 24 bits of their significands, but to 2^-133 at
+ * best; a product is off by less than 2^-24 of itself before it is summed (one within 2^-7 of the largest number may come out infinite).  An operand
  * that is not finite makes the results that it enters not finite, NaN or infinite (rows of other groups, and rows past the last, enter none).
  * No atomics: the same call gives the same bits.  n = 0 is allowed (A, G and transform_grouped's out may then be null).
  * wgrad_grouped needs device scratch of _scratch bytes, 256-byte aligned, that no other call uses until it is done; nothing in

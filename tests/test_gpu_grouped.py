@@ -489,6 +489,31 @@ def test_every_product_of_two_fp32_numbers(solver, rows):
             assert far.max() < 4 * 2.0 ** -24, (far.max() * 2.0 ** 24, np.unravel_index(far.argmax(), far.shape))
 
 
+@pytest.mark.parametrize("kind,small,large", [("f32", -100, 90), ("f32", -126, 100), ("f32", -140, 120), ("f32", -60, -60), ("bf16", -126, 100), ("bf16", -132, 110), ("f16", -15, 4),
+                                              ("f16", -20, 8)])
+@pytest.mark.parametrize("n,K,width", [(64, 64, 64), (5, 1, 40), (300, 256, 200), (9, 33, 5)])
+def test_operands_near_the_least_numbers(solver, kind, small, large, n, K, width):
+    """16-bit operands count as they are, subnormal ones too; the last part of an fp32 number is cut at 2^-133, bf16's least, which the
+    other operand multiplies."""
+    import torch
+    rng = np.random.default_rng(55)
+    A = torch.from_numpy(rng.standard_normal((n, K)) * 2.0 ** small).to(types()[kind])
+    B = torch.from_numpy(rng.standard_normal((1, K, width)) * 2.0 ** large).to(types()[kind])
+    ptr = torch.tensor([0, n])
+    want, size = want_nn(A, B, ptr, False)
+    cut = 2.0 ** -133 * 2.0 ** 24 / (K + 8)                   # (as close counts: times (K + 8) 2^-24)
+    if kind == "f32":
+        size = size + cut * (np.abs(B[0].double().numpy()).sum(0)[None, :] + A.double().abs().sum(1, keepdim=True).numpy())
+    close(solver.op_transform_grouped(A.cuda(), B.cuda(), ptr.cuda()), want, size, K, kind)
+    close(solver.op_transform_grouped(A.cuda(), B.transpose(1, 2).contiguous().cuda(), ptr.cuda(), transposed=True), want, size, K, kind)
+    G = B[:, 0].expand(n, width).contiguous() * torch.from_numpy(rng.choice([-1.0, 1.0], (n, 1))).to(B.dtype)
+    want, size = want_tn(A, G, ptr)
+    if kind == "f32":
+        cut = 2.0 ** -133 * 2.0 ** 24 / (n + 8)
+        size = size + cut * (G.double().abs().sum(0).numpy()[None, None, :] + A.double().abs().sum(0).numpy()[None, :, None])
+    close(solver.op_wgrad_grouped(A.cuda(), G.cuda(), ptr.cuda()), want, size, n, "f32")
+
+
 def test_no_rows_at_all(solver):
     import torch
     ptr = torch.zeros(4, dtype=torch.int64, device="cuda")
