@@ -524,11 +524,14 @@ class Solver:
             groups = group_ptr.shape[0] - 1
             self._refuse("op_transform_grouped", types, [("A", A, None, None)] + ([] if out is None else [("out", out, (n, cols), dtype)]),
                          [("group_ptr", group_ptr, (groups + 1,), (torch.int64,)), ("B", B, (groups, cols, K) if transposed else (groups, K, cols), (dtype,))])
-        if given:
-            self._apart("op_transform_grouped", out, ldo, ("A", A, lda), ("B", B, None), ("group_ptr", group_ptr, None))
+        a, b, p, o = A.data_ptr(), B.data_ptr(), group_ptr.data_ptr(), out.data_ptr()
+        if given:                                             # (looked at closely only if their stretches of memory meet)
+            size = 4 if dtype == torch.float32 else 2
+            end = o + size * ((n - 1) * ldo + cols)
+            if (o < a + size * ((n - 1) * lda + K) and a < end) or (o < b + size * groups * K * cols and b < end) or (o < p + 8 * groups + 8 and p < end):
+                self._apart("op_transform_grouped", out, ldo, ("A", A, lda), ("B", B, None), ("group_ptr", group_ptr, None))
         self._on_raw_stream()
-        rc = self.lib.cadmm_op_transform_grouped(self.h, types[dtype], A.data_ptr(), n, lda, K, B.data_ptr(), cols, 1 if transposed else 0, groups,
-                                                 group_ptr.data_ptr(), out.data_ptr(), ldo)
+        rc = self.lib.cadmm_op_transform_grouped(self.h, types[dtype], a, n, lda, K, b, cols, 1 if transposed else 0, groups, p, o, ldo)
         if rc:
             self._check(rc, "cadmm_op_transform_grouped")
         return out
@@ -554,12 +557,14 @@ class Solver:
         if not fits:
             self._refuse("op_wgrad_grouped", types, [("A", A, None, None), ("G", G, (n, width), dtype)],
                          [("group_ptr", group_ptr, (groups + 1,), (torch.int64,))] + ([] if out is None else [("out", out, (groups, K, width), wanted)]))
-        if given:
-            self._apart("op_wgrad_grouped", out, None, ("A", A, lda), ("G", G, ldg), ("group_ptr", group_ptr, None))
+        a, d, p, o = A.data_ptr(), G.data_ptr(), group_ptr.data_ptr(), out.data_ptr()
+        if given:                                             # (looked at closely only if their stretches of memory meet)
+            size, end = 4 if dtype == torch.float32 else 2, o + (4 if out.dtype == torch.float32 else 2) * groups * K * width
+            if (o < a + size * ((n - 1) * lda + K) and a < end) or (o < d + size * ((n - 1) * ldg + width) and d < end) or (o < p + 8 * groups + 8 and p < end):
+                self._apart("op_wgrad_grouped", out, None, ("A", A, lda), ("G", G, ldg), ("group_ptr", group_ptr, None))
         ptr, nbytes, hold = self._scratch(self.lib.cadmm_op_wgrad_grouped_scratch, n, K, width, groups)
         self._on_raw_stream()
-        rc = self.lib.cadmm_op_wgrad_grouped(self.h, types[dtype], A.data_ptr(), n, lda, K, G.data_ptr(), ldg, width, groups,
-                                             group_ptr.data_ptr(), types[out.dtype], out.data_ptr(), ptr, nbytes)
+        rc = self.lib.cadmm_op_wgrad_grouped(self.h, types[dtype], a, n, lda, K, d, ldg, width, groups, p, types[out.dtype], o, ptr, nbytes)
         if rc:
             self._check(rc, "cadmm_op_wgrad_grouped")
         return out
